@@ -42,7 +42,8 @@
 #include <stdint.h>
 
 /* Version of this interface: 2 added archead_pack_create_ex and
- * archead_abi_version.  archead_desc only grows by appending fields. */
+ * archead_abi_version.  archead_desc only grows by appending fields; new
+ * functions (the INT8 product, beam search) leave the version as it is. */
 #define ARCHEAD_ABI_VERSION 2
 
 #if defined(__GNUC__)
@@ -71,6 +72,14 @@ typedef enum {
   ARCHEAD_OUT_BF16 = 0, /* logits rounded to bf16 (nearest even) from fp32 accumulators */
   ARCHEAD_OUT_FP32 = 1  /* logits as the fp32 accumulators                               */
 } archead_out_dtype;
+
+/* Element types of the INT8 product and of beam search (below); the first two
+ * have the numbers of archead_out_dtype. */
+typedef enum {
+  ARCHEAD_DTYPE_BF16 = 0,
+  ARCHEAD_DTYPE_FP32 = 1,
+  ARCHEAD_DTYPE_FP16 = 2
+} archead_dtype;
 
 /* Stored format of the packed head (archead_desc.format). */
 typedef enum {
@@ -390,6 +399,137 @@ ARCHEAD_API archead_status archead_dequant_symmetric(const int8_t *codes, const 
 ARCHEAD_API archead_status archead_dequant_residual_sc4(const int8_t *codes, const uint8_t *scale_codes,
                                                         const uint16_t *row_scale, int64_t rows, int64_t cols,
                                                         int group_size, float *out, void *stream);
+
+/*
+ * Matrix product in 8-bit integers with a scale for each token and each
+ * output channel: the paper's "Row INT8" head (Section 4, "Baselines and
+ * implementation") with 8-bit activations, or a projection before the head.
+ *
+ *   y[m][n] = (sum_k x_codes[m][k] * codes[n][k]) * x_scales[m] * scales[n]
+ *
+ * A weight holds its codes in the kernels' layout and serves one stream at a
+ * time, like a pack: it owns the scratch of its calls (converted token codes
+ * and partial sums), which grows on demand after a device synchronisation (in a
+ * stream that is being captured a call that would need more answers
+ * ARCHEAD_ERR_UNSUPPORTED).  A call leaves room for every AUTO call with fewer
+ * tokens; a new weight has room for 64.
+ *
+ * archead_int8_weight_create: codes int8 [N][K] and scales fp32 [N] (host or
+ *   device memory, any alignment, read during the call only; the call waits
+ *   for the stream).  N >= 1, 1 <= K < 2^17 (the exact sum fits 32 bits for
+ *   any codes, -128 included); ARCHEAD_ERR_UNSUPPORTED for more than 2^31 -
+ *   256 channels.  On failure *out is NULL.
+ * archead_int8_quantize_tokens: codes int8 [M][K] and scales fp32 [M] of x
+ *   [M] rows of K elements of type `dtype`, ldx elements apart (ldx >= K):
+ *   scale = max|x| / 127, code = clamp(rint(x / scale), -127, 127), both
+ *   divisions in fp32, ties to even; code 0 where the scale is 0 or not
+ *   finite.  A row that holds a NaN or an infinity has that scale and codes
+ *   of 0, so its products are NaN.  x must be aligned to its elements, codes
+ *   and scales to 16 bytes.  Runs on the current device.
+ * archead_int8_matmul: x_codes int8 [M][K], x_scales fp32 [M] -> y [M] rows
+ *   of N elements of type out_dtype, ldy elements apart (ldy >= N).  Device
+ *   pointers, 16-byte aligned (y: also the rows' distance may be any).
+ *   Sums of products are exact integers while they stay below 2^24, and are
+ *   rounded to fp32 beyond (up to 8 tokens they are exact whatever their
+ *   size, and rounded once); then times x_scales[m], times scales[n], each
+ *   rounded to fp32, and rounded once to out_dtype.
+ * archead_int8_linear: the product of activations x as
+ *   archead_int8_quantize_tokens takes them (16-byte aligned) with the
+ *   weight: the same result as quantisation and product after one another.
+ * archead_int8_matmul_path: the product with an explicit kernel (tests,
+ *   crossover sweeps): ARCHEAD_PATH_DECODE the warp-level kernel,
+ *   ARCHEAD_PATH_PREFILL the tensor-memory kernel.
+ * archead_int8_sync_status: waits for the stream, then reads and clears the
+ *   weight's device error word (ARCHEAD_ERR_DEVICE_TIMEOUT: a pipeline wait
+ *   gave up).  archead_int8_set_wait_budget: as archead_set_wait_budget.
+ * archead_int8_device_bytes: device memory the weight holds now (-1: NULL).
+ */
+typedef struct archead_int8_weight archead_int8_weight; /* opaque, owned by the library */
+
+ARCHEAD_API archead_status archead_int8_weight_create(const int8_t *codes, const float *scales, int64_t N, int64_t K,
+                                                      void *stream, archead_int8_weight **out);
+ARCHEAD_API void archead_int8_weight_destroy(archead_int8_weight *weight);
+ARCHEAD_API int64_t archead_int8_device_bytes(const archead_int8_weight *weight);
+ARCHEAD_API archead_status archead_int8_quantize_tokens(const void *x, archead_dtype dtype, int64_t M, int64_t K,
+                                                        int64_t ldx, int8_t *codes, float *scales, void *stream);
+ARCHEAD_API archead_status archead_int8_matmul(archead_int8_weight *weight, const int8_t *x_codes,
+                                               const float *x_scales, int64_t M, void *y, archead_dtype out_dtype,
+                                               int64_t ldy, void *stream);
+ARCHEAD_API archead_status archead_int8_matmul_path(archead_int8_weight *weight, const int8_t *x_codes,
+                                                    const float *x_scales, int64_t M, void *y,
+                                                    archead_dtype out_dtype, int64_t ldy, archead_path path,
+                                                    void *stream);
+ARCHEAD_API archead_status archead_int8_linear(archead_int8_weight *weight, const void *x, archead_dtype x_dtype,
+                                               int64_t M, int64_t ldx, void *y, archead_dtype out_dtype, int64_t ldy,
+                                               void *stream);
+ARCHEAD_API archead_status archead_int8_sync_status(archead_int8_weight *weight, void *stream);
+ARCHEAD_API archead_status archead_int8_set_wait_budget(archead_int8_weight *weight, int64_t cycles);
+
+/*
+ * Beam search: the selection of the next beams and the reordering of the
+ * decoder's states.  No paper counterpart; it is the other generation-time
+ * use of the head, beside archead_forward_argmax.
+ *
+ * archead_beam_create: scratch for selections over up to max_rows (batch x
+ *   beams) rows of up to max_vocab logits with up to max_out candidates, so
+ *   that a selection allocates nothing.  Serves one stream at a time.
+ *   1 <= max_out <= ARCHEAD_BEAM_MAX_OUT, max_vocab <= 2^30, max_rows <= 2^20.
+ * archead_beam_select: of each batch entry's candidates (beam k, token v)
+ *     value = (scores[b][k] - lse) + logits[b * beams + k][v],
+ *     lse = log sum_v exp(logits[...][v]),
+ *   the n_out largest, largest first: out_scores fp32 (the values),
+ *   out_parents int32 (k), out_tokens int32 (v), each [batch][n_out].  Equal
+ *   values: the lower beam first; candidates of one beam are ordered by their
+ *   logits and, where those are equal, the lower token first.  A beam with
+ *   ended[b][k] != 0 has one candidate, (k, end_token), of value
+ *   scores[b][k]; its logits are not read.  What is not finite is no candidate: tokens of
+ *   logit -inf (masked), beams of score -inf, and whole beams that hold a
+ *   logit NaN or +inf.  Where candidates run out the value is -inf, the
+ *   parent and the token -1.
+ *     logits   device, [batch * beams] rows of vocab elements of type dtype,
+ *              ld elements apart (ld >= vocab), aligned to their elements
+ *     scores   device, fp32 [batch][beams]; ended device, uint8 or NULL
+ *   1 <= beams <= ARCHEAD_BEAM_MAX_BEAMS; batch == 0 is a no-op.
+ * archead_beam_reorder: row b * beams + k of every state takes the contents
+ *   that row b * beams + parents[b][k] had before the call; a parent outside
+ *   [0, beams) leaves zeros.  A state is
+ *     outer (layers) x rows (batch * beams) x inner (heads) chunks,
+ *   chunk (o, r, i) at o * outer_stride + r * row_stride + i * inner_stride,
+ *   of which the first bytes + length * bytes_per_position bytes are moved:
+ *   a cache [layer][row][head][room][dim] has bytes_per_position = dim *
+ *   element size and bytes = 0, a state without positions has its size in
+ *   bytes.  Distances are in bytes, of any alignment.  out == NULL: in place
+ *   (rows that keep their contents are not touched); else a buffer of the
+ *   same layout that shares no memory with data.  What lies between the
+ *   chunks is not touched.  Chunks must not overlap
+ *   (ARCHEAD_ERR_INVALID_ARG where a chunk is longer than a distance).  One
+ *   launch for up to 48 states.  parents device, int32 [batch][beams], not
+ *   part of a state.  `states` is host memory, read during the call only.
+ *   Runs on the current device.
+ */
+#define ARCHEAD_BEAM_MAX_OUT 64
+#define ARCHEAD_BEAM_MAX_BEAMS 64
+
+typedef struct archead_beam archead_beam; /* opaque, owned by the library */
+
+typedef struct {
+  void *data;
+  void *out; /* NULL: in place */
+  int64_t outer, outer_stride;
+  int64_t row_stride;
+  int64_t inner, inner_stride;
+  int64_t bytes, bytes_per_position;
+} archead_beam_state;
+
+ARCHEAD_API archead_status archead_beam_create(int64_t max_rows, int64_t max_vocab, int max_out, archead_beam **out);
+ARCHEAD_API void archead_beam_destroy(archead_beam *beam);
+ARCHEAD_API archead_status archead_beam_select(archead_beam *beam, const void *logits, archead_dtype dtype,
+                                               int64_t batch, int beams, int64_t vocab, int64_t ld,
+                                               const float *scores, const uint8_t *ended, int32_t end_token,
+                                               int n_out, float *out_scores, int32_t *out_parents,
+                                               int32_t *out_tokens, void *stream);
+ARCHEAD_API archead_status archead_beam_reorder(const archead_beam_state *states, int count, const int32_t *parents,
+                                                int64_t batch, int beams, int64_t length, void *stream);
 
 /* Per-kernel timing with CUDA events on the launch stream (off by default). */
 typedef struct {

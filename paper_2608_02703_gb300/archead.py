@@ -31,6 +31,13 @@ OUT_FP32 = 1
 FORMAT_INT8 = 0
 FORMAT_SC4 = 1
 
+DTYPE_BF16 = 0
+DTYPE_FP32 = 1
+DTYPE_FP16 = 2
+
+BEAM_MAX_OUT = 64
+BEAM_MAX_BEAMS = 64
+
 PATH_AUTO = 0
 PATH_DECODE = 1
 PATH_PREFILL = 2
@@ -46,6 +53,10 @@ EXPORTED = (
     "archead_forward_lse_partial", "archead_lse_combine", "archead_argmax_combine",
     "archead_quantize_symmetric", "archead_quantize_residual_sc4", "archead_pack_codes", "archead_dequant_symmetric",
     "archead_dequant_residual_sc4", "archead_pack_create_ex", "archead_abi_version",
+    "archead_int8_weight_create", "archead_int8_weight_destroy", "archead_int8_device_bytes",
+    "archead_int8_quantize_tokens", "archead_int8_matmul", "archead_int8_matmul_path", "archead_int8_linear",
+    "archead_int8_sync_status", "archead_int8_set_wait_budget",
+    "archead_beam_create", "archead_beam_destroy", "archead_beam_select", "archead_beam_reorder",
 )
 
 
@@ -75,6 +86,15 @@ class archead_desc(ctypes.Structure):  # noqa: N801 - mirrors the C struct name
 
 class archead_kernel_stat(ctypes.Structure):  # noqa: N801
     _fields_ = [("name", ctypes.c_char_p), ("launches", ctypes.c_int64), ("total_ms", ctypes.c_double)]
+
+
+class archead_beam_state_t(ctypes.Structure):  # noqa: N801 - the C struct archead_beam_state
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("out", ctypes.c_void_p),
+        ("outer", ctypes.c_int64), ("outer_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+        ("inner", ctypes.c_int64), ("inner_stride", ctypes.c_int64),
+        ("bytes", ctypes.c_int64), ("bytes_per_position", ctypes.c_int64),
+    ]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -120,6 +140,19 @@ def load() -> ctypes.CDLL:
         "archead_sync_status": (i32, [vp, vp]),
         "archead_set_wait_budget": (i32, [vp, i64]),
         "archead_debug_wait_timeout": (i32, [vp, vp]),
+        "archead_int8_weight_create": (i32, [vp, vp, i64, i64, vp, ctypes.POINTER(vp)]),
+        "archead_int8_weight_destroy": (None, [vp]),
+        "archead_int8_device_bytes": (i64, [vp]),
+        "archead_int8_quantize_tokens": (i32, [vp, i32, i64, i64, i64, vp, vp, vp]),
+        "archead_int8_matmul": (i32, [vp, vp, vp, i64, vp, i32, i64, vp]),
+        "archead_int8_matmul_path": (i32, [vp, vp, vp, i64, vp, i32, i64, i32, vp]),
+        "archead_int8_linear": (i32, [vp, vp, i32, i64, i64, vp, i32, i64, vp]),
+        "archead_int8_sync_status": (i32, [vp, vp]),
+        "archead_int8_set_wait_budget": (i32, [vp, i64]),
+        "archead_beam_create": (i32, [i64, i64, i32, ctypes.POINTER(vp)]),
+        "archead_beam_destroy": (None, [vp]),
+        "archead_beam_select": (i32, [vp, vp, i32, i64, i32, i64, i64, vp, vp, ctypes.c_int32, i32, vp, vp, vp, vp]),
+        "archead_beam_reorder": (i32, [vp, i32, vp, i64, i32, i64, vp]),
         "archead_profile_enable": (i32, [vp, i32]),
         "archead_profile_read": (i32, [vp, ctypes.POINTER(archead_kernel_stat), i32]),
         "archead_status_string": (ctypes.c_char_p, [i32]),
@@ -310,6 +343,259 @@ def archead_dequant_residual_sc4(codes, scale_codes, row_scale, group_size: int,
     _check(load().archead_dequant_residual_sc4(_ptr(codes), _ptr(scale_codes), _ptr(row_scale), rows, cols,
                                                group_size, _ptr(out), _stream_ptr(stream)),
            "archead_dequant_residual_sc4")
+
+
+def _dtype(t) -> int:
+    import torch
+
+    codes = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, torch.float16: DTYPE_FP16}
+    if t.dtype not in codes:
+        raise ValueError(f"bf16, fp16 or fp32 is wanted, not {t.dtype}")
+    return codes[t.dtype]
+
+
+def _rows(t, rows: int, cols: int, what: str) -> int:
+    """Distance of the rows of a matrix of at least `rows` rows whose `cols` columns lie side by side."""
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: {rows} rows of {cols} adjacent elements are wanted, "
+                         f"not {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else cols
+
+
+def _flat(t, dtype, size: int, what: str):
+    """A contiguous tensor of at least `size` elements of the type."""
+    if t.dtype != dtype or t.numel() < size or not t.is_contiguous():
+        raise ValueError(f"{what}: {size} contiguous elements of {dtype} are wanted, not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+class Int8Weight:
+    """A weight matrix in 8-bit codes on one CUDA device (wraps archead_int8_weight*)."""
+
+    def __init__(self, handle: int, N: int, K: int):
+        self.handle = handle
+        self.N = N
+        self.K = K
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def close(self) -> None:
+        if self.handle:
+            load().archead_int8_weight_destroy(self.handle)
+            self.handle = None
+
+
+def archead_int8_weight_create(codes, scales, stream=None) -> Int8Weight:
+    """codes int8 [N, K] and scales fp32 [N]: numpy arrays or torch tensors, on the host or the device."""
+    N, K = codes.shape
+    if isinstance(codes, np.ndarray):
+        codes = np.ascontiguousarray(codes, dtype=np.int8)
+        scales = np.ascontiguousarray(scales, dtype=np.float32)
+        n_scales = scales.size
+    else:
+        import torch
+
+        if codes.dtype != torch.int8 or scales.dtype != torch.float32:
+            raise ValueError(f"codes in int8 and scales in fp32 are wanted, not {codes.dtype} and {scales.dtype}")
+        codes, scales = codes.contiguous(), scales.contiguous()
+        n_scales = scales.numel()
+    if n_scales != N:
+        raise ValueError(f"a scale for each of the {N} channels is wanted, not {n_scales}")
+    h = ctypes.c_void_p()
+    _check(load().archead_int8_weight_create(_ptr(codes), _ptr(scales), N, K, _stream_ptr(stream), ctypes.byref(h)),
+           "archead_int8_weight_create")
+    return Int8Weight(h.value, N, K)
+
+
+def archead_int8_weight_destroy(weight: Int8Weight) -> None:
+    weight.close()
+
+
+def archead_int8_device_bytes(weight: Int8Weight) -> int:
+    return int(load().archead_int8_device_bytes(weight.handle))
+
+
+def archead_int8_quantize_tokens(x, codes, scales, stream=None) -> None:
+    """codes int8 [M, K] and scales fp32 [M] of the rows of x (bf16, fp16 or fp32 [M, K], rows any distance apart)."""
+    import torch
+
+    M, K = x.shape
+    ldx = _rows(x, M, K, "x")
+    _check(load().archead_int8_quantize_tokens(x.data_ptr(), _dtype(x), M, K, ldx, _flat(codes, torch.int8, M * K, "codes"),
+                                               _flat(scales, torch.float32, M, "scales"), _stream_ptr(stream)),
+           "archead_int8_quantize_tokens")
+
+
+def archead_int8_matmul(weight: Int8Weight, x_codes, x_scales, M: int, y, stream=None) -> None:
+    """y [M, N] (bf16, fp16 or fp32, rows any distance apart) of int8 codes [M, K] and fp32 scales [M]."""
+    archead_int8_matmul_path(weight, x_codes, x_scales, M, y, PATH_AUTO, stream)
+
+
+def archead_int8_matmul_path(weight: Int8Weight, x_codes, x_scales, M: int, y, path: int, stream=None) -> None:
+    import torch
+
+    ldy = _rows(y, M, weight.N, "y")
+    _check(load().archead_int8_matmul_path(weight.handle, _flat(x_codes, torch.int8, M * weight.K, "x_codes"),
+                                           _flat(x_scales, torch.float32, M, "x_scales"), M, y.data_ptr(), _dtype(y),
+                                           ldy, path, _stream_ptr(stream)), "archead_int8_matmul")
+
+
+def archead_int8_linear(weight: Int8Weight, x, M: int, y, stream=None) -> None:
+    """y [M, N] of activations x [M, K], which the call quantises (each bf16, fp16 or fp32, rows any distance apart)."""
+    ldx, ldy = _rows(x, M, weight.K, "x"), _rows(y, M, weight.N, "y")
+    _check(load().archead_int8_linear(weight.handle, x.data_ptr(), _dtype(x), M, ldx, y.data_ptr(), _dtype(y), ldy,
+                                      _stream_ptr(stream)), "archead_int8_linear")
+
+
+def archead_int8_sync_status(weight: Int8Weight, stream=None) -> int:
+    return int(load().archead_int8_sync_status(weight.handle, _stream_ptr(stream)))
+
+
+def archead_int8_set_wait_budget(weight: Int8Weight, cycles: int) -> None:
+    _check(load().archead_int8_set_wait_budget(weight.handle, cycles), "archead_int8_set_wait_budget")
+
+
+class Beam:
+    """Scratch of beam selections on one CUDA device (wraps archead_beam*)."""
+
+    def __init__(self, handle: int):
+        self.handle = handle
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def close(self) -> None:
+        if self.handle:
+            load().archead_beam_destroy(self.handle)
+            self.handle = None
+
+
+def archead_beam_create(max_rows: int, max_vocab: int, max_out: int) -> Beam:
+    h = ctypes.c_void_p()
+    _check(load().archead_beam_create(max_rows, max_vocab, max_out, ctypes.byref(h)), "archead_beam_create")
+    return Beam(h.value)
+
+
+def archead_beam_destroy(beam: Beam) -> None:
+    beam.close()
+
+
+def archead_beam_select(beam: Beam, logits, scores, out_scores, out_parents, out_tokens, ended=None,
+                        end_token: int = 0, stream=None) -> None:
+    """The n best (beam, token) candidates of each batch entry.
+
+    logits [batch * beams, vocab] (bf16, fp16 or fp32, rows any distance apart), scores fp32 [batch, beams], ended
+    uint8 or bool [batch, beams] or None; out_scores fp32, out_parents and out_tokens int32, all [batch, n]."""
+    import torch
+
+    batch, beams = scores.shape
+    n = out_scores.shape[1]
+    vocab = logits.shape[1]
+    ld = _rows(logits, batch * beams, vocab, "logits")
+    if ended is not None and ended.dtype == torch.bool:
+        ended = ended.view(torch.uint8)
+    _check(load().archead_beam_select(
+        beam.handle, logits.data_ptr(), _dtype(logits), batch, beams, vocab, ld,
+        _flat(scores, torch.float32, batch * beams, "scores"),
+        None if ended is None else _flat(ended, torch.uint8, batch * beams, "ended"), end_token, n,
+        _flat(out_scores, torch.float32, batch * n, "out_scores"),
+        _flat(out_parents, torch.int32, batch * n, "out_parents"),
+        _flat(out_tokens, torch.int32, batch * n, "out_tokens"), _stream_ptr(stream)), "archead_beam_select")
+
+
+def _merged(shape, strides, what: str):
+    """Dimensions as one: their extent and stride."""
+    dims = [(n, s) for n, s in zip(shape, strides) if n != 1]
+    if any(n == 0 for n, _ in dims):
+        return 0, 0
+    for (_, s0), (n1, s1) in zip(dims, dims[1:]):
+        if s0 != n1 * s1:
+            raise ValueError(f"{what} of the state do not lie at one distance")
+    extent = 1
+    for n, _ in dims:
+        extent *= n
+    return extent, dims[-1][1] if dims else 0
+
+
+class BeamState:
+    """One state as archead_beam_reorder takes it: its description, its rows and the positions it has room for."""
+
+    def __init__(self, desc, rows, room, tensors):
+        self.desc = desc
+        self.rows = rows
+        self.room = room  # None: no positions
+        self.tensors = tensors
+
+
+def archead_beam_state(t, row_dim: int = 0, length_dim: Optional[int] = None, out=None) -> BeamState:
+    """Describes a state [layers..., rows, heads..., positions, elements...]: rows = batch * beams in dimension
+    row_dim, positions (of which a reordering moves the first `length`) in dimension length_dim, or none.  out: a
+    tensor of the same shape and strides that takes the result; None: in place."""
+    if out is not None and (out.shape != t.shape or out.stride() != t.stride() or out.dtype != t.dtype):
+        raise ValueError("out is not laid out as the state")
+    shape, strides, size = list(t.shape), list(t.stride()), t.element_size()
+    row_dim %= t.dim()
+    if length_dim is None:
+        # The dimensions that lie side by side at the end are one chunk.
+        tail, run = t.dim(), 1
+        while tail - 1 > row_dim and (shape[tail - 1] == 1 or strides[tail - 1] == run):
+            tail -= 1
+            run *= shape[tail]
+        room, fixed, step = None, run * size, 0
+    else:
+        tail = length_dim % t.dim()
+        if tail <= row_dim:
+            raise ValueError("the positions' dimension comes after the rows'")
+        run = 1
+        for n, s in zip(reversed(shape[tail + 1:]), reversed(strides[tail + 1:])):
+            if n != 1 and s != run:
+                raise ValueError("a position's elements do not lie side by side")
+            run *= n
+        room, fixed, step = shape[tail], 0, run * size
+        if room > 1 and strides[tail] != run:
+            raise ValueError("the positions do not lie side by side")
+    outer, outer_stride = _merged(shape[:row_dim], strides[:row_dim], "the dimensions before the rows")
+    inner, inner_stride = _merged(shape[row_dim + 1:tail], strides[row_dim + 1:tail], "the dimensions after the rows")
+    desc = archead_beam_state_t(
+        data=t.data_ptr(), out=None if out is None else out.data_ptr(), outer=outer, outer_stride=outer_stride * size,
+        row_stride=strides[row_dim] * size, inner=inner, inner_stride=inner_stride * size, bytes=fixed,
+        bytes_per_position=step)
+    return BeamState(desc, shape[row_dim], room, (t, out))
+
+
+class BeamStates:
+    """The states of a decoder, described once: what archead_beam_reorder takes."""
+
+    def __init__(self, states: List[BeamState]):
+        self.array = (archead_beam_state_t * max(len(states), 1))(*[s.desc for s in states])
+        self.count = len(states)
+        self.rows = min((s.rows for s in states), default=0)
+        self.room = min((s.room for s in states if s.room is not None), default=None)
+        self.tensors = [s.tensors for s in states]  # (their memory is kept)
+
+
+def archead_beam_states(states: List[BeamState]) -> BeamStates:
+    return BeamStates(list(states))
+
+
+def archead_beam_reorder(states: BeamStates, parents, length: int = 0, stream=None) -> None:
+    """Row b * beams + k of every state takes what row b * beams + parents[b, k] held (parents int32 [batch, beams]),
+    for the first `length` positions of states that have positions."""
+    import torch
+
+    batch, beams = parents.shape
+    if states.count and (batch * beams > states.rows or (states.room is not None and length > states.room)):
+        raise ValueError(f"{batch * beams} rows of {length} positions in states of {states.rows} rows and "
+                         f"{states.room} positions")
+    _check(load().archead_beam_reorder(states.array, states.count, _flat(parents, torch.int32, batch * beams, "parents"),
+                                       batch, beams, length, _stream_ptr(stream)), "archead_beam_reorder")
 
 
 def archead_pack_bytes(pack: Pack) -> int:

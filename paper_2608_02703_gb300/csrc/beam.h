@@ -1,0 +1,62 @@
+// Internal definitions of beam search (beam_*.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "archead.h"
+
+struct archead_beam {
+  int device = 0;
+  int sm_count = 0;
+  int64_t max_rows = 0, max_vocab = 0;
+  int max_out = 0;
+  void *ws = nullptr;
+};
+
+namespace archead {
+
+// A row of logits is cut into slices; a slice leaves (max, sum of exp(l - max))
+// and its n best (logit, token) keys, best first.
+struct SelectParams {
+  const void *logits;
+  int64_t ld;
+  int rows, beams, vocab, n;
+  const float *scores;
+  const uint8_t *ended;  // may be NULL
+  int32_t end_token;
+  int slices, slice_len;
+  float2 *part;     // [rows][slices]
+  uint64_t *keys;   // [rows][slices][n]
+  float *out_scores;
+  int32_t *out_parents, *out_tokens;
+};
+
+// Slices that a selection cuts each row into, and the scratch of the largest one.
+int beam_slices(int64_t rows, int64_t vocab, int sm_count);
+size_t beam_scratch_bytes(int64_t max_rows, int max_out, int sm_count);
+
+cudaError_t launch_beam_select(SelectParams p, int dtype, int64_t batch, void *ws, int sm_count, cudaStream_t s);
+
+constexpr int kReorderStates = 48;  // states of one launch
+struct ReorderState {
+  const char *src;
+  char *dst;
+  int64_t outer_stride, row_stride, inner_stride;
+  int64_t total;       // vectors of one row
+  int64_t chunk;       // vectors of a chunk
+  int inner;
+  int width;           // bytes of a vector
+  int first_tile;      // tiles of the states before this one
+};
+struct ReorderParams {
+  ReorderState st[kReorderStates];
+  const int32_t *parents;
+  int64_t batch;
+  int beams, count, tiles, place;
+};
+cudaError_t launch_beam_reorder(const ReorderParams &p, cudaStream_t s);
+int reorder_vector_bytes(int beams);  // most bytes a thread moves of each row
+constexpr int kReorderTile = 256;     // vectors of a row that a block moves
+
+}  // namespace archead

@@ -1,0 +1,150 @@
+// C entry points of beam search (include/archead.h): argument checks and launches.
+#include <algorithm>
+#include <new>
+
+#include "beam.h"
+#include "status.h"
+
+using namespace archead;
+
+namespace {
+
+// The largest power of two up to 16 that divides v.
+int64_t low_bits(int64_t v) { return v == 0 ? 16 : std::min<int64_t>(v & -v, 16); }
+
+}  // namespace
+
+extern "C" {
+
+archead_status archead_beam_create(int64_t max_rows, int64_t max_vocab, int max_out, archead_beam **out) {
+  if (!out) return ARCHEAD_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (max_rows < 1 || max_vocab < 1 || max_out < 1 || max_out > ARCHEAD_BEAM_MAX_OUT) return ARCHEAD_ERR_INVALID_ARG;
+  if (max_rows > 1 << 20 || max_vocab > 1 << 30) return ARCHEAD_ERR_UNSUPPORTED;
+  archead_beam *b = new (std::nothrow) archead_beam();
+  if (!b) return ARCHEAD_ERR_OOM;
+  b->max_rows = max_rows;
+  b->max_vocab = max_vocab;
+  b->max_out = max_out;
+  cudaError_t e = cudaGetDevice(&b->device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&b->sm_count, cudaDevAttrMultiProcessorCount, b->device);
+  if (e == cudaSuccess) e = cudaMalloc(&b->ws, beam_scratch_bytes(max_rows, max_out, b->sm_count));
+  if (e != cudaSuccess) {
+    delete b;
+    return status_of(e);
+  }
+  *out = b;
+  return ARCHEAD_OK;
+}
+
+void archead_beam_destroy(archead_beam *b) {
+  if (!b) return;
+  cudaSetDevice(b->device);
+  cudaDeviceSynchronize();
+  cudaFree(b->ws);
+  delete b;
+}
+
+archead_status archead_beam_select(archead_beam *beam, const void *logits, archead_dtype dtype, int64_t batch,
+                                   int beams, int64_t vocab, int64_t ld, const float *scores, const uint8_t *ended,
+                                   int32_t end_token, int n_out, float *out_scores, int32_t *out_parents,
+                                   int32_t *out_tokens, void *stream) {
+  if (!beam || !is_dtype(dtype) || batch < 0 || beams < 1 || beams > ARCHEAD_BEAM_MAX_BEAMS || vocab < 1 ||
+      ld < vocab || n_out < 1)
+    return ARCHEAD_ERR_INVALID_ARG;
+  if (batch == 0) return ARCHEAD_OK;
+  if (!logits || !scores || !out_scores || !out_parents || !out_tokens || !is_aligned(logits, dtype_bytes(dtype)) ||
+      !is_aligned(scores, 4) || !is_aligned(out_scores, 4) || !is_aligned(out_parents, 4) || !is_aligned(out_tokens, 4))
+    return ARCHEAD_ERR_INVALID_ARG;
+  if (batch > beam->max_rows / beams || vocab > beam->max_vocab || n_out > beam->max_out) {
+    set_last_error_message("the selection is larger than its scratch was created for");
+    return ARCHEAD_ERR_UNSUPPORTED;
+  }
+  AH_TRY(cudaSetDevice(beam->device));
+  SelectParams p{};
+  p.logits = logits;
+  p.ld = ld;
+  p.rows = (int)(batch * beams);
+  p.beams = beams;
+  p.vocab = (int)vocab;
+  p.n = n_out;
+  p.scores = scores;
+  p.ended = ended;
+  p.end_token = end_token;
+  p.out_scores = out_scores;
+  p.out_parents = out_parents;
+  p.out_tokens = out_tokens;
+  AH_TRY(launch_beam_select(p, dtype, batch, beam->ws, beam->sm_count, static_cast<cudaStream_t>(stream)));
+  return ARCHEAD_OK;
+}
+
+archead_status archead_beam_reorder(const archead_beam_state *states, int count, const int32_t *parents, int64_t batch,
+                                    int beams, int64_t length, void *stream) {
+  if (count < 0 || batch < 0 || beams < 1 || beams > ARCHEAD_BEAM_MAX_BEAMS || length < 0)
+    return ARCHEAD_ERR_INVALID_ARG;
+  if (count == 0 || batch == 0) return ARCHEAD_OK;
+  if (!states || !parents || !is_aligned(parents, 4)) return ARCHEAD_ERR_INVALID_ARG;
+  if (batch > (int64_t)1 << 30) return ARCHEAD_ERR_UNSUPPORTED;
+  const int64_t rows = batch * beams;
+  // Every state is checked before the first is moved.
+  for (int i = 0; i < count; ++i) {
+    const archead_beam_state &a = states[i];
+    if (a.outer < 0 || a.inner < 0 || a.bytes < 0 || a.bytes_per_position < 0 || a.outer_stride < 0 ||
+        a.row_stride < 0 || a.inner_stride < 0 || a.inner > 0x7fffffff)
+      return ARCHEAD_ERR_INVALID_ARG;
+    int64_t all;
+    if (__builtin_mul_overflow(a.outer, a.inner, &all)) return ARCHEAD_ERR_INVALID_ARG;
+    constexpr int64_t kMost = (int64_t)1 << 46;  // keeps the products below in 64 bits
+    if (a.bytes > kMost || a.bytes_per_position > kMost / std::max<int64_t>(length, 1)) return ARCHEAD_ERR_INVALID_ARG;
+    const int64_t bytes = a.bytes + length * a.bytes_per_position;
+    if (__builtin_mul_overflow(all, bytes, &all)) return ARCHEAD_ERR_INVALID_ARG;
+    if (all == 0) continue;
+    if (!a.data || a.out == a.data) return ARCHEAD_ERR_INVALID_ARG;
+    if ((a.outer > 1 && bytes > a.outer_stride) || (rows > 1 && bytes > a.row_stride) ||
+        (a.inner > 1 && bytes > a.inner_stride))
+      return ARCHEAD_ERR_INVALID_ARG;
+  }
+  const int most = reorder_vector_bytes(beams);
+  ReorderParams p;
+  p.parents = parents;
+  p.batch = batch;
+  p.beams = beams;
+  int i = 0;
+  while (i < count) {
+    // In place and into another buffer are launches of their own.
+    p.count = 0;
+    p.place = states[i].out == nullptr;
+    int64_t tiles = 0;
+    for (; i < count && p.count < kReorderStates && (states[i].out == nullptr) == (p.place != 0); ++i) {
+      const archead_beam_state &a = states[i];
+      const int64_t bytes = a.bytes + length * a.bytes_per_position;
+      if (bytes == 0 || a.outer == 0 || a.inner == 0) continue;
+      char *dst = static_cast<char *>(p.place ? a.data : a.out);
+      const int64_t width = std::min<int64_t>(
+          {(int64_t)most, low_bits((int64_t)(intptr_t)a.data), low_bits((int64_t)(intptr_t)dst), low_bits(bytes),
+           a.outer > 1 ? low_bits(a.outer_stride) : 16, rows > 1 ? low_bits(a.row_stride) : 16,
+           a.inner > 1 ? low_bits(a.inner_stride) : 16});
+      ReorderState &st = p.st[p.count];
+      st.src = static_cast<const char *>(a.data);
+      st.dst = dst;
+      st.outer_stride = a.outer_stride;
+      st.row_stride = a.row_stride;
+      st.inner_stride = a.inner_stride;
+      st.inner = (int)a.inner;
+      st.width = (int)width;
+      st.chunk = bytes / width;
+      st.total = st.chunk * a.inner * a.outer;
+      const int64_t n = (st.total + kReorderTile - 1) / kReorderTile;
+      if (n > 0x7fffffff) return ARCHEAD_ERR_UNSUPPORTED;
+      if (tiles + n > 0x7fffffff) break;  // the next launch
+      st.first_tile = (int)tiles;
+      tiles += n;
+      ++p.count;
+    }
+    p.tiles = (int)tiles;
+    if (p.count > 0) AH_TRY(launch_beam_reorder(p, static_cast<cudaStream_t>(stream)));
+  }
+  return ARCHEAD_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,93 @@
+// Reordering of the decoder's states: row b * beams + k of each state takes
+// what row b * beams + parents[b][k] held before (include/archead.h).
+//
+// Memory bound.  A thread takes one vector (up to 16 bytes) of a row's place
+// for all beams of a batch entry: it reads the vectors of the parents and then
+// writes those of the rows that change, so that the exchange needs no second
+// buffer and no order among blocks.  In place, rows that keep their contents
+// are neither read (unless another beam takes them) nor written; a parent that several
+// beams take comes from the first-level cache the second time.
+#include <algorithm>
+
+#include "beam.h"
+
+namespace archead {
+
+namespace {
+
+template <int kMax, typename T>
+__device__ __forceinline__ void move_rows(const ReorderState &st, const int *parent, int beams, bool place, int64_t row0,
+                                          int64_t offset, T zero) {
+  const char *src = st.src + row0 * st.row_stride + offset;
+  char *dst = st.dst + row0 * st.row_stride + offset;
+  T v[kMax];
+#pragma unroll
+  for (int k = 0; k < kMax; ++k) {
+    v[k] = zero;
+    if (k < beams) {
+      const int q = parent[k];
+      if (q >= 0 && !(place && q == k)) v[k] = *reinterpret_cast<const T *>(src + q * st.row_stride);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kMax; ++k)
+    if (k < beams && !(place && parent[k] == k)) *reinterpret_cast<T *>(dst + k * st.row_stride) = v[k];
+}
+
+template <int kMax>
+__global__ void __launch_bounds__(kReorderTile) beam_reorder_kernel(const __grid_constant__ ReorderParams p) {
+  __shared__ int parent[kMax];
+  const int tile = blockIdx.x;
+  int lo = 0, hi = p.count - 1;  // the last state whose first tile is not after this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.st[mid].first_tile <= tile) lo = mid;
+    else hi = mid - 1;
+  }
+  const ReorderState &st = p.st[lo];
+  const int64_t v = (int64_t)(tile - st.first_tile) * kReorderTile + threadIdx.x;
+  const int64_t per = st.chunk * st.inner;
+  const int64_t o = v / per, in = v - o * per, i = in / st.chunk;
+  const int64_t offset = o * st.outer_stride + i * st.inner_stride + (in - i * st.chunk) * st.width;
+  for (int64_t b = blockIdx.y; b < p.batch; b += gridDim.y) {
+    __syncthreads();
+    int q = -1;
+    if (threadIdx.x < p.beams) {
+      q = p.parents[b * p.beams + threadIdx.x];
+      if (q < 0 || q >= p.beams) q = -1;
+      parent[threadIdx.x] = q;
+    }
+    if (!__syncthreads_or(threadIdx.x < p.beams && !(p.place && q == (int)threadIdx.x))) continue;
+    if (v >= st.total) continue;
+    const int64_t row0 = b * p.beams;
+    if (kMax <= 16 && st.width == 16)
+      move_rows<kMax>(st, parent, p.beams, p.place, row0, offset, make_uint4(0, 0, 0, 0));
+    else if (kMax <= 32 && st.width == 8)
+      move_rows<kMax>(st, parent, p.beams, p.place, row0, offset, make_uint2(0, 0));
+    else if (st.width == 4)
+      move_rows<kMax>(st, parent, p.beams, p.place, row0, offset, 0u);
+    else if (st.width == 2)
+      move_rows<kMax>(st, parent, p.beams, p.place, row0, offset, (uint16_t)0);
+    else
+      move_rows<kMax>(st, parent, p.beams, p.place, row0, offset, (uint8_t)0);
+  }
+}
+
+}  // namespace
+
+int reorder_vector_bytes(int beams) { return beams <= 16 ? 16 : beams <= 32 ? 8 : 4; }
+
+cudaError_t launch_beam_reorder(const ReorderParams &p, cudaStream_t s) {
+  const dim3 grid(p.tiles, (unsigned)std::min<int64_t>(p.batch, 65535));
+  const auto run = [&](auto kern) {
+    kern<<<grid, kReorderTile, 0, s>>>(p);
+    return cudaGetLastError();
+  };
+  return p.beams <= 4    ? run(beam_reorder_kernel<4>)
+         : p.beams <= 8  ? run(beam_reorder_kernel<8>)
+         : p.beams <= 16 ? run(beam_reorder_kernel<16>)
+         : p.beams <= 32 ? run(beam_reorder_kernel<32>)
+                         : run(beam_reorder_kernel<64>);
+}
+
+}  // namespace archead

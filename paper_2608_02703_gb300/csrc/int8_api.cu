@@ -1,0 +1,216 @@
+// C entry points of the INT8 product (include/archead.h): argument checks, the
+// weight handle and its workspace, kernel sequencing.
+#include <new>
+
+#include "device.cuh"
+#include "int8.h"
+#include "internal.h"
+#include "status.h"
+
+using namespace archead;
+
+namespace {
+
+constexpr int kReserveTokens = 64;  // a new weight's workspace
+
+struct Plan {
+  size_t x_off = 0, scale_off = 0, total = 0;
+};
+
+size_t take(size_t &off, size_t bytes) {
+  const size_t o = off;
+  off += (bytes + 255) / 256 * 256;
+  return o;
+}
+
+Plan plan(const archead_int8_weight *w, int64_t M) {
+  Plan p;
+  p.x_off = take(p.total, (size_t)M * w->K_pad);
+  p.scale_off = take(p.total, (size_t)M * sizeof(float));
+  return p;
+}
+
+// Growing synchronises the device: a call made earlier on another stream may
+// still use the old buffer.
+cudaError_t grow_workspace(archead_int8_weight *w, size_t bytes) {
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return e;
+  if (w->ws) {
+    cudaFree(w->ws);
+    w->owned_bytes -= (int64_t)w->ws_bytes;
+    w->ws = nullptr;
+    w->ws_bytes = 0;
+  }
+  e = cudaMalloc(&w->ws, bytes);
+  if (e != cudaSuccess) return e;
+  w->ws_bytes = bytes;
+  w->owned_bytes += (int64_t)bytes;
+  return cudaSuccess;
+}
+
+archead_status ensure_workspace(archead_int8_weight *w, size_t bytes, cudaStream_t s) {
+  if (bytes <= w->ws_bytes) return ARCHEAD_OK;
+  if (is_capturing(s)) {
+    set_last_error_message("the workspace cannot grow while the stream is captured: call once with as many tokens before");
+    return ARCHEAD_ERR_UNSUPPORTED;
+  }
+  return status_of(grow_workspace(w, bytes));
+}
+
+template <typename T>
+T *at(const archead_int8_weight *w, size_t off) {
+  return reinterpret_cast<T *>(static_cast<char *>(w->ws) + off);
+}
+
+void free_weight(archead_int8_weight *w) {
+  for (void *b : {(void *)w->codes, (void *)w->scales, (void *)w->err, w->ws})
+    if (b) cudaFree(b);
+  delete w;
+}
+
+archead_status check_product(const archead_int8_weight *w, const void *x, int64_t M, const void *y, int out_dtype,
+                             int64_t ldy) {
+  if (!w || M < 0 || !is_dtype(out_dtype) || ldy < w->N) return ARCHEAD_ERR_INVALID_ARG;
+  if (M == 0) return ARCHEAD_OK;
+  if (!x || !y || !is_aligned(x, 16) || !is_aligned(y, 16)) return ARCHEAD_ERR_INVALID_ARG;
+  if (M > (int64_t)1 << 30) return ARCHEAD_ERR_UNSUPPORTED;
+  return ARCHEAD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+archead_status archead_int8_weight_create(const int8_t *codes, const float *scales, int64_t N, int64_t K, void *stream,
+                                          archead_int8_weight **out) {
+  if (!out) return ARCHEAD_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!codes || !scales || N < 1 || K < 1) return ARCHEAD_ERR_INVALID_ARG;
+  if (K > kI8MaxK || N > ((int64_t)1 << 31) - 256) return ARCHEAD_ERR_UNSUPPORTED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  archead_int8_weight *w = new (std::nothrow) archead_int8_weight();
+  if (!w) return ARCHEAD_ERR_OOM;
+  int8_t *staged = nullptr;
+  const auto build = [&]() -> cudaError_t {
+    cudaError_t e = cudaGetDevice(&w->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&w->sm_count, cudaDevAttrMultiProcessorCount, w->device);
+    if (e != cudaSuccess) return e;
+    w->N = N;
+    w->K = (int)K;
+    w->N_pad = (N + kI8PadN - 1) / kI8PadN * kI8PadN;
+    w->K_pad = (int)((K + kI8PadK - 1) / kI8PadK * kI8PadK);
+    w->wait_budget = kDefaultWaitBudget;
+    const size_t code_bytes = (size_t)w->N_pad * w->K_pad, scale_bytes = (size_t)w->N_pad * sizeof(float);
+    if ((e = cudaMalloc(&w->codes, code_bytes)) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&w->scales, scale_bytes)) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&w->err, 16)) != cudaSuccess) return e;
+    w->owned_bytes = (int64_t)(code_bytes + scale_bytes + 16);
+    if ((e = grow_workspace(w, plan(w, kReserveTokens).total)) != cudaSuccess) return e;
+    if ((e = cudaMemsetAsync(w->err, 0, 16, s)) != cudaSuccess) return e;
+    if ((e = cudaMemsetAsync(w->scales, 0, scale_bytes, s)) != cudaSuccess) return e;
+    if ((e = cudaMemcpyAsync(w->scales, scales, (size_t)N * sizeof(float), cudaMemcpyDefault, s)) != cudaSuccess)
+      return e;
+    // Codes in this device's memory are re-tiled from where they are.
+    const int8_t *src = codes;
+    cudaPointerAttributes attr{};
+    const bool known = cudaPointerGetAttributes(&attr, codes) == cudaSuccess;
+    cudaGetLastError();
+    if (!known || attr.type != cudaMemoryTypeDevice || attr.device != w->device) {
+      if ((e = cudaMalloc(&staged, (size_t)(N * K))) != cudaSuccess) return e;
+      if ((e = cudaMemcpyAsync(staged, codes, (size_t)(N * K), cudaMemcpyDefault, s)) != cudaSuccess) return e;
+      src = staged;
+    }
+    if ((e = launch_int8_layout(w, src, s)) != cudaSuccess) return e;
+    return cudaStreamSynchronize(s);
+  };
+  const cudaError_t e = build();
+  if (staged) cudaFree(staged);
+  if (e != cudaSuccess) {
+    const archead_status st = status_of(e);
+    free_weight(w);
+    return st;
+  }
+  *out = w;
+  return ARCHEAD_OK;
+}
+
+void archead_int8_weight_destroy(archead_int8_weight *w) {
+  if (!w) return;
+  cudaSetDevice(w->device);
+  cudaDeviceSynchronize();
+  free_weight(w);
+}
+
+int64_t archead_int8_device_bytes(const archead_int8_weight *w) { return w ? w->owned_bytes : -1; }
+
+archead_status archead_int8_quantize_tokens(const void *x, archead_dtype dtype, int64_t M, int64_t K, int64_t ldx,
+                                            int8_t *codes, float *scales, void *stream) {
+  if (M < 0 || K < 1 || ldx < K || !is_dtype(dtype)) return ARCHEAD_ERR_INVALID_ARG;
+  if (M == 0) return ARCHEAD_OK;
+  if (!x || !codes || !scales || !is_aligned(x, dtype_bytes(dtype)) || !is_aligned(codes, 16) ||
+      !is_aligned(scales, 16))
+    return ARCHEAD_ERR_INVALID_ARG;
+  if (M > (int64_t)1 << 30 || K > (int64_t)1 << 30) return ARCHEAD_ERR_UNSUPPORTED;
+  AH_TRY(launch_int8_quantize(x, dtype, M, K, ldx, codes, K, K, scales, static_cast<cudaStream_t>(stream)));
+  return ARCHEAD_OK;
+}
+
+archead_status archead_int8_matmul_path(archead_int8_weight *w, const int8_t *x_codes, const float *x_scales,
+                                        int64_t M, void *y, archead_dtype out_dtype, int64_t ldy, archead_path path,
+                                        void *stream) {
+  archead_status st = check_product(w, x_codes, M, y, out_dtype, ldy);
+  if (st != ARCHEAD_OK || M == 0) return st;
+  if (!x_scales || !is_aligned(x_scales, 16)) return ARCHEAD_ERR_INVALID_ARG;
+  if (path != ARCHEAD_PATH_AUTO && path != ARCHEAD_PATH_DECODE && path != ARCHEAD_PATH_PREFILL)
+    return ARCHEAD_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  AH_TRY(cudaSetDevice(w->device));
+  const Plan p = plan(w, M);
+  if ((st = ensure_workspace(w, p.total, s)) != ARCHEAD_OK) return st;
+  int8_t *x = at<int8_t>(w, p.x_off);
+  AH_TRY(launch_int8_pad(x_codes, M, w->K, w->K_pad, x, s));
+  AH_TRY(launch_int8_product(w, x, x_scales, M, {y, ldy, out_dtype}, s));
+  return ARCHEAD_OK;
+}
+
+archead_status archead_int8_matmul(archead_int8_weight *w, const int8_t *x_codes, const float *x_scales, int64_t M,
+                                   void *y, archead_dtype out_dtype, int64_t ldy, void *stream) {
+  return archead_int8_matmul_path(w, x_codes, x_scales, M, y, out_dtype, ldy, ARCHEAD_PATH_AUTO, stream);
+}
+
+archead_status archead_int8_linear(archead_int8_weight *w, const void *x, archead_dtype x_dtype, int64_t M,
+                                   int64_t ldx, void *y, archead_dtype out_dtype, int64_t ldy, void *stream) {
+  archead_status st = check_product(w, x, M, y, out_dtype, ldy);
+  if (st != ARCHEAD_OK) return st;
+  if (!is_dtype(x_dtype) || ldx < w->K) return ARCHEAD_ERR_INVALID_ARG;
+  if (M == 0) return ARCHEAD_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  AH_TRY(cudaSetDevice(w->device));
+  const Plan p = plan(w, M);
+  if ((st = ensure_workspace(w, p.total, s)) != ARCHEAD_OK) return st;
+  int8_t *q = at<int8_t>(w, p.x_off);
+  float *sc = at<float>(w, p.scale_off);
+  AH_TRY(launch_int8_quantize(x, x_dtype, M, w->K, ldx, q, w->K_pad, w->K_pad, sc, s));
+  AH_TRY(launch_int8_product(w, q, sc, M, {y, ldy, out_dtype}, s));
+  return ARCHEAD_OK;
+}
+
+archead_status archead_int8_sync_status(archead_int8_weight *w, void *stream) {
+  if (!w) return ARCHEAD_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  AH_TRY(cudaSetDevice(w->device));
+  AH_TRY(cudaStreamSynchronize(s));
+  int word = 0;
+  AH_TRY(cudaMemcpyAsync(&word, w->err, sizeof(int), cudaMemcpyDeviceToHost, s));
+  AH_TRY(cudaStreamSynchronize(s));
+  AH_TRY(cudaMemsetAsync(w->err, 0, sizeof(int), s));
+  return word & kErrWaitTimeout ? ARCHEAD_ERR_DEVICE_TIMEOUT : ARCHEAD_OK;
+}
+
+archead_status archead_int8_set_wait_budget(archead_int8_weight *w, int64_t cycles) {
+  if (!w || cycles <= 0) return ARCHEAD_ERR_INVALID_ARG;
+  w->wait_budget = cycles;
+  return ARCHEAD_OK;
+}
+
+}  // extern "C"
