@@ -2,16 +2,21 @@
 // its device layout and the kernel launchers.
 //
 //  Codes, "fragment-native".  The channels (N padded with zero rows to N_PAD,
-//  a multiple of 128) are cut into strips of 16, K (padded with zero codes to
-//  K_PAD, a multiple of 128) into blocks of 32.  Block (strip, kb) is 512
-//  bytes: [lane 0..31][word j 0..3] of 32-bit words, a strip's blocks following
-//  one another.  Word j of lane (gq = lane/4, cq = lane%4) holds row 16 strip +
-//  gq + 8 (j & 1), columns 32 kb + 8 cq + 4 (j >> 1) + 0..3, lowest first: the
-//  four registers of an m16n8k32 A fragment, if the columns of a block are
-//  taken in that order (any order serves a sum, if both operands share it).
-//  The same words, two codes at a time, are the A fragments of two m16n8k16
-//  steps.
-//    byte offset = ((strip * KB + kb) * 32 + lane) * 16 + 4 j,   KB = K_PAD/32
+//  a multiple of 128) are cut into tiles of 128 and these into strips of 16, K
+//  (padded with zero codes to K_PAD, a multiple of 128) into stages of 128 and
+//  these into blocks of 32.  A (tile, stage) is 16 KB, one bulk copy: [strip
+//  0..7][block 0..3][lane 0..31][word j 0..3] of 32-bit words.  Word j of lane
+//  (gq = lane/4, cq = lane%4) holds row 16 strip + gq + 8 (j & 1) of the tile,
+//  columns 8 cq + 4 (j >> 1) + 0..3 of the block, lowest first: the four
+//  registers of an m16n8k32 A fragment, if the columns of a block are taken in
+//  that order (any order serves a sum, if both operands share it).  The same
+//  words, two codes at a time, are the A fragments of two m16n8k16 steps.
+//    byte offset = ((((tile * KC + stage) * 8 + strip) * 4 + block) * 32 + lane) * 16 + 4 j,   KC = K_PAD/128
+//
+//  Token codes, widened to fp16 for the tensor-memory kernel: [M][K_PAD] in
+//  the same order of K.  Of the eight columns 8 cq + 0..7 of a block, pair i
+//  (columns 8 cq + 2 i, + 1) is word 4 i + cq of the block's 16 words: k16 step
+//  i >> 1, fragment registers 2 (i & 1) and its neighbour.
 //
 //  Scales: fp32 [N_PAD], zero on padding rows.
 #pragma once
@@ -30,18 +35,19 @@ struct archead_int8_weight {
   uint8_t *codes = nullptr;
   float *scales = nullptr;
   int *err = nullptr;
+  int *counters = nullptr;  // of the K slices (zero between calls)
   void *ws = nullptr;
   size_t ws_bytes = 0;
+  int64_t reserved_tokens = 0;  // every AUTO call of up to so many fits
   int64_t owned_bytes = 0;
   int64_t wait_budget = 0;
 };
 
 namespace archead {
 
-constexpr int kI8Strip = 16;        // channels per strip
-constexpr int kI8Block = 32;        // K per block
-constexpr int kI8BlockBytes = 512;  // codes of a block
-constexpr int kI8PadN = 128, kI8PadK = 128;
+constexpr int kI8Strip = 16;  // channels per strip
+constexpr int kI8Block = 32;  // K per block
+constexpr int kI8PadN = 128, kI8PadK = 128;  // a tile's channels, a stage's K
 constexpr int kI8MaxK = (1 << 17) - 1;
 
 // Output rows: y[m][n] at y + (m * ld + n) elements.
@@ -53,14 +59,26 @@ struct I8Out {
 
 cudaError_t launch_int8_layout(const archead_int8_weight *w, const int8_t *codes, cudaStream_t s);
 
-// Quantisation of M rows of K elements.  Codes go to rows of ldc bytes, of
-// which [K, k_fill) are set to zero.
-cudaError_t launch_int8_quantize(const void *x, int dtype, int64_t M, int64_t K, int64_t ldx, int8_t *codes,
+// Quantisation of M rows of K elements.  Codes go to rows of ldc codes, of
+// which [K, k_fill) are set to zero; wide: to rows of k_fill widened codes
+// (k_fill a multiple of 128).
+cudaError_t launch_int8_quantize(const void *x, int dtype, int64_t M, int64_t K, int64_t ldx, void *codes, bool wide,
                                  int64_t ldc, int64_t k_fill, float *scales, cudaStream_t s);
-// Token codes [M][K] into rows of K_pad bytes, zero beyond K.
-cudaError_t launch_int8_pad(const int8_t *codes, int64_t M, int K, int K_pad, int8_t *out, cudaStream_t s);
+// Token codes [M][K] into rows of K_pad codes (wide: widened), zero beyond K.
+cudaError_t launch_int8_pad(const int8_t *codes, int64_t M, int K, int K_pad, void *out, bool wide, cudaStream_t s);
 // Product of padded token codes with the weight.
 cudaError_t launch_int8_product(const archead_int8_weight *w, const int8_t *x, const float *x_scales, int64_t M,
                                 I8Out out, cudaStream_t s);
+
+// Tensor-memory kernel: how a product of M tokens is cut.
+struct I8GemmPlan {
+  int NT = 0, nt = 0, ks = 1;
+  int64_t num_mt = 0, units = 0;
+  size_t partial_bytes = 0;
+};
+I8GemmPlan int8_gemm_plan(const archead_int8_weight *w, int64_t M);
+// x: widened token codes [M][K_pad]; partial: scratch of the plan's size.
+cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, const uint16_t *x,
+                             const float *x_scales, int64_t M, I8Out out, float *partial, cudaStream_t s);
 
 }  // namespace archead

@@ -1,5 +1,6 @@
 // C entry points of the INT8 product (include/archead.h): argument checks, the
 // weight handle and its workspace, kernel sequencing.
+#include <algorithm>
 #include <new>
 
 #include "device.cuh"
@@ -13,8 +14,11 @@ namespace {
 
 constexpr int kReserveTokens = 64;  // a new weight's workspace
 
+// A call's kernel and its place in the workspace.
 struct Plan {
-  size_t x_off = 0, scale_off = 0, total = 0;
+  bool gemm = false;
+  I8GemmPlan g;
+  size_t x_off = 0, scale_off = 0, partial_off = 0, total = 0;
 };
 
 size_t take(size_t &off, size_t bytes) {
@@ -23,11 +27,28 @@ size_t take(size_t &off, size_t bytes) {
   return o;
 }
 
-Plan plan(const archead_int8_weight *w, int64_t M) {
+// AUTO: the warp-level kernel up to 16 tokens, the tensor-memory kernel above.
+constexpr int kDecodeTokens = 16;
+
+Plan plan(const archead_int8_weight *w, int64_t M, archead_path path) {
   Plan p;
-  p.x_off = take(p.total, (size_t)M * w->K_pad);
+  p.gemm = path == ARCHEAD_PATH_PREFILL || (path == ARCHEAD_PATH_AUTO && M > kDecodeTokens);
+  p.x_off = take(p.total, (size_t)M * w->K_pad * (p.gemm ? 2 : 1));
   p.scale_off = take(p.total, (size_t)M * sizeof(float));
+  if (p.gemm) {
+    p.g = int8_gemm_plan(w, M);
+    p.partial_off = take(p.total, p.g.partial_bytes);
+  }
   return p;
+}
+
+// The most that AUTO needs for up to M tokens.  K slices have the most partial
+// sums at the largest count of a tokens' tile.
+size_t room_for(const archead_int8_weight *w, int64_t M) {
+  size_t most = 0;
+  for (int64_t m : {(int64_t)16, (int64_t)32, (int64_t)48, (int64_t)64, (int64_t)128, (int64_t)256, (int64_t)512, (int64_t)1024})
+    if (m < M) most = std::max(most, plan(w, m, ARCHEAD_PATH_AUTO).total);
+  return std::max(most, plan(w, M, ARCHEAD_PATH_AUTO).total);
 }
 
 // Growing synchronises the device: a call made earlier on another stream may
@@ -48,7 +69,13 @@ cudaError_t grow_workspace(archead_int8_weight *w, size_t bytes) {
   return cudaSuccess;
 }
 
-archead_status ensure_workspace(archead_int8_weight *w, size_t bytes, cudaStream_t s) {
+// Room for a call that needs `bytes`, and for every AUTO call of fewer tokens.
+archead_status ensure_workspace(archead_int8_weight *w, size_t bytes, int64_t M, cudaStream_t s) {
+  if (bytes <= w->ws_bytes && M <= w->reserved_tokens) return ARCHEAD_OK;
+  if (M > w->reserved_tokens && !is_capturing(s)) {
+    bytes = std::max(bytes, room_for(w, M));
+    w->reserved_tokens = M;
+  }
   if (bytes <= w->ws_bytes) return ARCHEAD_OK;
   if (is_capturing(s)) {
     set_last_error_message("the workspace cannot grow while the stream is captured: call once with as many tokens before");
@@ -62,8 +89,19 @@ T *at(const archead_int8_weight *w, size_t off) {
   return reinterpret_cast<T *>(static_cast<char *>(w->ws) + off);
 }
 
+// One for each epilogue warp of the (tile, tokens) that K slices may share.
+size_t counter_bytes(const archead_int8_weight *w) { return (size_t)w->sm_count * 8 * sizeof(int); }
+
+// The product of token codes that have been laid out in the workspace.
+archead_status run_product(archead_int8_weight *w, const Plan &p, const float *x_scales, int64_t M, I8Out out,
+                           cudaStream_t s) {
+  if (p.gemm)
+    return status_of(launch_int8_gemm(w, p.g, at<uint16_t>(w, p.x_off), x_scales, M, out, at<float>(w, p.partial_off), s));
+  return status_of(launch_int8_product(w, at<int8_t>(w, p.x_off), x_scales, M, out, s));
+}
+
 void free_weight(archead_int8_weight *w) {
-  for (void *b : {(void *)w->codes, (void *)w->scales, (void *)w->err, w->ws})
+  for (void *b : {(void *)w->codes, (void *)w->scales, (void *)w->err, (void *)w->counters, w->ws})
     if (b) cudaFree(b);
   delete w;
 }
@@ -100,12 +138,16 @@ archead_status archead_int8_weight_create(const int8_t *codes, const float *scal
     w->N_pad = (N + kI8PadN - 1) / kI8PadN * kI8PadN;
     w->K_pad = (int)((K + kI8PadK - 1) / kI8PadK * kI8PadK);
     w->wait_budget = kDefaultWaitBudget;
+    w->reserved_tokens = kReserveTokens;
     const size_t code_bytes = (size_t)w->N_pad * w->K_pad, scale_bytes = (size_t)w->N_pad * sizeof(float);
     if ((e = cudaMalloc(&w->codes, code_bytes)) != cudaSuccess) return e;
     if ((e = cudaMalloc(&w->scales, scale_bytes)) != cudaSuccess) return e;
     if ((e = cudaMalloc(&w->err, 16)) != cudaSuccess) return e;
     w->owned_bytes = (int64_t)(code_bytes + scale_bytes + 16);
-    if ((e = grow_workspace(w, plan(w, kReserveTokens).total)) != cudaSuccess) return e;
+    if ((e = grow_workspace(w, room_for(w, kReserveTokens))) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&w->counters, counter_bytes(w))) != cudaSuccess) return e;
+    w->owned_bytes += (int64_t)counter_bytes(w);
+    if ((e = cudaMemsetAsync(w->counters, 0, counter_bytes(w), s)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(w->err, 0, 16, s)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(w->scales, 0, scale_bytes, s)) != cudaSuccess) return e;
     if ((e = cudaMemcpyAsync(w->scales, scales, (size_t)N * sizeof(float), cudaMemcpyDefault, s)) != cudaSuccess)
@@ -151,7 +193,7 @@ archead_status archead_int8_quantize_tokens(const void *x, archead_dtype dtype, 
       !is_aligned(scales, 16))
     return ARCHEAD_ERR_INVALID_ARG;
   if (M > (int64_t)1 << 30 || K > (int64_t)1 << 30) return ARCHEAD_ERR_UNSUPPORTED;
-  AH_TRY(launch_int8_quantize(x, dtype, M, K, ldx, codes, K, K, scales, static_cast<cudaStream_t>(stream)));
+  AH_TRY(launch_int8_quantize(x, dtype, M, K, ldx, codes, false, K, K, scales, static_cast<cudaStream_t>(stream)));
   return ARCHEAD_OK;
 }
 
@@ -165,12 +207,10 @@ archead_status archead_int8_matmul_path(archead_int8_weight *w, const int8_t *x_
     return ARCHEAD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_TRY(cudaSetDevice(w->device));
-  const Plan p = plan(w, M);
-  if ((st = ensure_workspace(w, p.total, s)) != ARCHEAD_OK) return st;
-  int8_t *x = at<int8_t>(w, p.x_off);
-  AH_TRY(launch_int8_pad(x_codes, M, w->K, w->K_pad, x, s));
-  AH_TRY(launch_int8_product(w, x, x_scales, M, {y, ldy, out_dtype}, s));
-  return ARCHEAD_OK;
+  const Plan p = plan(w, M, path);
+  if ((st = ensure_workspace(w, p.total, M, s)) != ARCHEAD_OK) return st;
+  AH_TRY(launch_int8_pad(x_codes, M, w->K, w->K_pad, at<void>(w, p.x_off), p.gemm, s));
+  return run_product(w, p, x_scales, M, {y, ldy, out_dtype}, s);
 }
 
 archead_status archead_int8_matmul(archead_int8_weight *w, const int8_t *x_codes, const float *x_scales, int64_t M,
@@ -186,13 +226,11 @@ archead_status archead_int8_linear(archead_int8_weight *w, const void *x, archea
   if (M == 0) return ARCHEAD_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_TRY(cudaSetDevice(w->device));
-  const Plan p = plan(w, M);
-  if ((st = ensure_workspace(w, p.total, s)) != ARCHEAD_OK) return st;
-  int8_t *q = at<int8_t>(w, p.x_off);
-  float *sc = at<float>(w, p.scale_off);
-  AH_TRY(launch_int8_quantize(x, x_dtype, M, w->K, ldx, q, w->K_pad, w->K_pad, sc, s));
-  AH_TRY(launch_int8_product(w, q, sc, M, {y, ldy, out_dtype}, s));
-  return ARCHEAD_OK;
+  const Plan p = plan(w, M, ARCHEAD_PATH_AUTO);
+  if ((st = ensure_workspace(w, p.total, M, s)) != ARCHEAD_OK) return st;
+  float *scales = at<float>(w, p.scale_off);
+  AH_TRY(launch_int8_quantize(x, x_dtype, M, w->K, ldx, at<void>(w, p.x_off), p.gemm, w->K_pad, w->K_pad, scales, s));
+  return run_product(w, p, scales, M, {y, ldy, out_dtype}, s);
 }
 
 archead_status archead_int8_sync_status(archead_int8_weight *w, void *stream) {
@@ -204,7 +242,14 @@ archead_status archead_int8_sync_status(archead_int8_weight *w, void *stream) {
   AH_TRY(cudaMemcpyAsync(&word, w->err, sizeof(int), cudaMemcpyDeviceToHost, s));
   AH_TRY(cudaStreamSynchronize(s));
   AH_TRY(cudaMemsetAsync(w->err, 0, sizeof(int), s));
-  return word & kErrWaitTimeout ? ARCHEAD_ERR_DEVICE_TIMEOUT : ARCHEAD_OK;
+  if (word & kErrLayout) {
+    set_last_error_message("a kernel found its shared-memory window misaligned for its TMA layout and skipped its work");
+    return ARCHEAD_ERR_UNSUPPORTED;
+  }
+  if (!(word & kErrWaitTimeout)) return ARCHEAD_OK;
+  // A call that gave up may have left its counters behind.
+  AH_TRY(cudaMemsetAsync(w->counters, 0, counter_bytes(w), s));
+  return ARCHEAD_ERR_DEVICE_TIMEOUT;
 }
 
 archead_status archead_int8_set_wait_budget(archead_int8_weight *w, int64_t cycles) {

@@ -1,0 +1,417 @@
+// Tensor-memory kernel of the INT8 product: more tokens than the warp-level
+// kernel takes.
+//
+// 8-bit codes are exact in fp16, and this chip's tensor cores do fp16 products
+// far faster than 8-bit integer ones (warp-level: 299 against 75 T
+// multiply-adds a second), so the kernel runs kind::f16 MMAs on widened codes.
+// Products are integers up to 2^14 and their fp32 sums exact up to 2^24.
+//
+// The weight's 128 channels of a tile are the MMA's M side (one TMEM lane
+// each), the tokens its N side.  Per stage of 128 of K:
+//   - one warp loads the tokens' widened codes (fp16, in the K order of the
+//     weight's words, 128-byte swizzle) by TMA, another the tile's 16 KB of
+//     codes with one bulk copy;
+//   - a converter warpgroup (several take stages in turn) widens the codes and
+//     stores them as the A operand in tensor memory, whose tcgen05.st.16x128b
+//     registers are the fragment registers that the words hold;
+//   - one thread issues eight MMAs into a TMEM accumulator that holds the whole
+//     K of the unit;
+//   - epilogue warps read the accumulator, scale, round and store.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "int8.h"
+#include "prefill_kernel.cuh"  // tcgen05 wrappers, ring positions
+
+namespace archead {
+
+// Instance for units of up to NT tokens.  TMEM: kAcc accumulators of NT
+// columns, then kA stages of the A operand (64 columns: 128 of K).
+template <int NT>
+struct I8Geom {
+  static constexpr int kAcc = 256 / NT;
+  static constexpr int kConv = NT == 256 ? 2 : 4;  // converter warpgroups
+  static constexpr int kA = 4;                     // A stages
+  static constexpr int kEpi = NT == 64 ? 1 : 2;    // epilogue warpgroups
+  static constexpr int kCols = NT / kEpi;          // accumulator columns a thread takes
+  static constexpr int kThreads = 128 * (1 + kConv + kEpi);
+  static constexpr int kBoxBytes = NT * 64 * 2;
+  static constexpr int kXBytes = 2 * kBoxBytes;
+  static constexpr int kXS = NT == 64 ? 6 : NT == 128 ? 4 : 2;
+  static constexpr int kCodeSlot = kI8PadN * kI8PadK;  // 16 KB
+  static constexpr int kCS = NT == 64 ? 7 : 5;
+  static constexpr int kCodeOff = kXS * kXBytes;
+  static constexpr int kBarOff = kCodeOff + kCS * kCodeSlot;
+  static constexpr int kBars = 2 * kXS + 2 * kCS + 2 * kA + 2 * kAcc + 1;
+  static constexpr int kSmem = kBarOff + kBars * 8 + 16;
+  static constexpr int kRegs0 = NT == 256 ? 48 : 56;
+  static constexpr int kRegsC = NT == 64 ? 72 : 56;
+  static constexpr int kRegsP = NT == 64 ? 128 : NT == 128 ? 112 : 160;
+  static_assert(128 * (kRegs0 + kConv * kRegsC + kEpi * kRegsP) <= 65536 / kThreads / 8 * 8 * kThreads, "registers");
+  static_assert(kAcc * NT + kA * 64 <= kPfTmemCols, "TMEM columns");
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+  static_assert(kCS >= kA, "code slots (see the converters)");
+};
+
+struct I8GemmParams {
+  CUtensorMap tmap_x;  // fp16 [M][K_pad], box 64 x nt
+  const uint8_t *codes;
+  const float *scales, *x_scales;
+  I8Out out;
+  int64_t N;
+  int M, nt, num_mt, units;
+  int KC;    // stages of K
+  int ks;    // slices of K (units of their own, joined through `partial`)
+  float *partial;
+  int *counters;  // one a warp of each (tile, tokens), zero between calls
+  int *err;
+  int64_t wait_budget;
+};
+
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n) {
+  return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// Four signed codes as two fp16 pairs, exact: the offset-binary byte u in the
+// mantissa of fp16 1024 is 1024 + u = 1152 + code.
+__device__ __forceinline__ void widen_int8x4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+  const uint32_t u = w ^ 0x80808080u;
+  const __half2 bias = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
+  const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+  const __half2 ra = __hsub2(*reinterpret_cast<const __half2 *>(&a), bias);
+  const __half2 rb = __hsub2(*reinterpret_cast<const __half2 *>(&b), bias);
+  lo = *reinterpret_cast<const uint32_t *>(&ra);
+  hi = *reinterpret_cast<const uint32_t *>(&rb);
+}
+
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// One channel's sums of kCols tokens, of which `cols` are there.
+template <typename T, int kCols>
+__device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_t n, const float (&acc)[kCols], int cols,
+                                              const float *x_scales, float sw) {
+  T *y = static_cast<T *>(o.y) + m0 * o.ld + n;
+#pragma unroll
+  for (int i = 0; i < kCols; ++i, y += o.ld)
+    if (i < cols) *y = from_f32<T>(acc[i] * x_scales[m0 + i] * sw);
+}
+
+template <int NT>
+__global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(const __grid_constant__ I8GemmParams p) {
+  using G = I8Geom<NT>;
+  constexpr int kXS = G::kXS, kCS = G::kCS, kA = G::kA, kAcc = G::kAcc;
+  extern __shared__ uint8_t smem[];  // 1024-byte aligned (the swizzle's period)
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + G::kBarOff);
+  uint64_t *x_full = bars, *x_empty = x_full + kXS, *c_full = x_empty + kXS, *c_empty = c_full + kCS;
+  uint64_t *a_full = c_empty + kCS, *a_empty = a_full + kA, *acc_full = a_empty + kA, *acc_empty = acc_full + kAcc;
+  uint64_t *drain = acc_empty + kAcc;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = lane_id();
+
+  if (smem_u32(smem) & 1023) {  // the same for every block: nothing has been started
+    if (threadIdx.x == 0) atomicOr(p.err, kErrLayout);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kXS; ++i) mbar_init(&x_full[i], 1), mbar_init(&x_empty[i], 1);
+    for (int i = 0; i < kCS; ++i) mbar_init(&c_full[i], 1), mbar_init(&c_empty[i], 4);
+    for (int i = 0; i < kA; ++i) mbar_init(&a_full[i], 4), mbar_init(&a_empty[i], 1);
+    for (int i = 0; i < kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4 * G::kEpi);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, kPfTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t a_base = tmem_base + kAcc * NT;
+  bool mma_leader = false;
+
+  // Unit u: K slice u % ks, tokens (u / ks) % num_mt, tile u / ks / num_mt.
+  const auto k_begin = [&](int u) { return (int)((int64_t)p.KC * (u % p.ks) / p.ks); };
+  const auto k_end = [&](int u) { return (int)((int64_t)p.KC * (u % p.ks + 1) / p.ks); };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegs0) : "memory");
+    if (warp == 0) {
+      // ------------------------------ tokens ------------------------------
+      const bool leader = elect_one();
+      RingPos<kXS> r;
+      int issued = 0;
+      asm volatile("griddepcontrol.wait;\n" ::: "memory");  // the widened codes come from the grid before
+      for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
+        const int m0 = u / p.ks % p.num_mt * p.nt, end = k_end(u);
+        for (int e = k_begin(u); e < end; ++e) {
+          if (!mbar_wait_warp(&x_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
+            drain_copies(x_full, kXS, issued, p.wait_budget, p.err);
+            goto done;
+          }
+          if (leader) {
+            uint8_t *dst = smem + r.s * G::kXBytes;
+            mbar_arrive_expect_tx(&x_full[r.s], (uint32_t)p.nt * 256);
+            tma_load_2d(dst, &p.tmap_x, e * 128, m0, &x_full[r.s]);
+            tma_load_2d(dst + G::kBoxBytes, &p.tmap_x, e * 128 + 64, m0, &x_full[r.s]);
+          }
+          ++issued;
+          r.next();
+          __syncwarp();
+        }
+      }
+    } else if (warp == 2) {
+      // ------------------------------ weight codes ------------------------------
+      const bool leader = elect_one();
+      RingPos<kCS> r;
+      int issued = 0;
+      for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
+        const uint8_t *src = p.codes + (int64_t)(u / p.ks / p.num_mt) * p.KC * G::kCodeSlot;
+        const int end = k_end(u);
+        for (int e = k_begin(u); e < end; ++e) {
+          if (!mbar_wait_warp(&c_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
+            drain_copies(c_full, kCS, issued, p.wait_budget, p.err);
+            goto done;
+          }
+          if (leader) {
+            mbar_arrive_expect_tx(&c_full[r.s], G::kCodeSlot);
+            bulk_g2s(smem + G::kCodeOff + r.s * G::kCodeSlot, src + (int64_t)e * G::kCodeSlot, G::kCodeSlot,
+                     &c_full[r.s]);
+          }
+          ++issued;
+          r.next();
+          __syncwarp();
+        }
+      }
+    } else if (warp == 1) {
+      // ------------------------------ MMAs ------------------------------
+      const bool leader = elect_one();
+      mma_leader = leader;
+      const uint32_t idesc = idesc_f16(128, p.nt);
+      const uint64_t xdesc = smem_desc_sw128(smem_u32(smem));
+      constexpr uint32_t kBox = G::kBoxBytes >> 4;
+      RingPos<kXS> xr;
+      RingPos<kA> ar;
+      RingPos<kAcc> accr;
+      for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
+        const int begin = k_begin(u), end = k_end(u);
+        if (!mbar_wait_warp(&acc_empty[accr.s], accr.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
+        const uint32_t d = tmem_base + accr.s * NT;
+        for (int e = begin; e < end; ++e) {
+          if (!mbar_wait_warp(&x_full[xr.s], xr.ph, p.wait_budget, abort_flag, p.err)) goto done;
+          if (!mbar_wait_warp(&a_full[ar.s], ar.ph, p.wait_budget, abort_flag, p.err)) goto done;
+          tc_fence_after();
+          if (leader) {
+            const uint32_t a = a_base + ar.s * 64;
+            const uint64_t b = xdesc + (uint32_t)(xr.s * (G::kXBytes >> 4));
+#pragma unroll
+            for (int q = 0; q < 8; ++q)  // (+2 in the descriptor: 32 bytes)
+              tc_mma_ts(d, a + 8 * q, b + (q >> 2) * kBox + 2 * (q & 3), idesc, q > 0 || e > begin);
+            tc_commit(&x_empty[xr.s]);
+            tc_commit(&a_empty[ar.s]);
+            if (e + 1 == end) tc_commit(&acc_full[accr.s]);
+          }
+          __syncwarp();
+          xr.next();
+          ar.next();
+        }
+        accr.next();
+      }
+    }
+  } else if (warp < 4 + 4 * G::kConv) {
+    // ------------------------------ converters ------------------------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegsC) : "memory");
+    const int cg = (warp - 4) >> 2, cw = warp & 3;
+    RingPos<kCS> cr;
+    RingPos<kA> ar;
+    cr.next(cg);
+    ar.next(cg);
+    int n = cg;  // this warpgroup's next stage, of the stages of unit u
+    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
+      const int len = k_end(u) - k_begin(u);
+      for (; n < len; n += G::kConv) {
+        // The A stage first: that it is free says that all stages up to n - kA
+        // are converted, so with kCS >= kA slots the code slot's barrier is at
+        // most one phase from this stage's (a parity shows no more).
+        if (!mbar_wait_warp(&a_empty[ar.s], ar.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
+        if (!mbar_wait_warp(&c_full[cr.s], cr.ph, p.wait_budget, abort_flag, p.err)) goto done;
+        tc_fence_after();
+        const uint4 *codes = reinterpret_cast<const uint4 *>(smem + G::kCodeOff + cr.s * G::kCodeSlot) + cw * 256 + lane;
+        const uint32_t acol = a_base + ((uint32_t)(cw * 32) << 16) + ar.s * 64;
+        uint4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = codes[32 * i];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // the warp's strips of 16 channels
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {  // 64 of K: four steps of 16
+            uint32_t a[16];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint4 v = w[2 * half + i];
+              widen_int8x4(v.x, a[8 * i], a[8 * i + 2]);
+              widen_int8x4(v.y, a[8 * i + 1], a[8 * i + 3]);
+              widen_int8x4(v.z, a[8 * i + 4], a[8 * i + 6]);
+              widen_int8x4(v.w, a[8 * i + 5], a[8 * i + 7]);
+              if (h == 0) w[2 * half + i] = codes[128 + 32 * (2 * half + i)];
+            }
+            tmem_st_frag4(acol + ((uint32_t)(16 * h) << 16) + 32 * half, a);
+          }
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c_empty[cr.s]), mbar_arrive(&a_full[ar.s]);
+        cr.next(G::kConv);
+        ar.next(G::kConv % kA);
+        if (G::kConv == kA) ar.ph ^= 1;
+      }
+      n -= len;
+    }
+  } else {
+    // ------------------------------ epilogue ------------------------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(G::kRegsP) : "memory");
+    constexpr int kCols = G::kCols;
+    const int pw = (warp - 4 - 4 * G::kConv) >> 2, lg = warp & 3;
+    const int col0 = kCols * pw;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(lg * 32) << 16) + col0;
+    RingPos<kAcc> accr;
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");  // (the tokens' scales)
+    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
+      const int t = u / p.ks, slice = u % p.ks;
+      const int64_t n = (int64_t)(t / p.num_mt) * kI8PadN + lg * 32 + lane;
+      const int mu = t % p.num_mt * p.nt;
+      const int m0 = mu + col0, cols = min(kCols, min(p.M, mu + p.nt) - m0);  // (may be negative: none)
+      const float sw = p.scales[n];
+      if (!mbar_wait_warp(&acc_full[accr.s], accr.ph, p.wait_budget, abort_flag, p.err)) goto done;
+      tc_fence_after();
+      float acc[kCols];
+#pragma unroll
+      for (int c = 0; c < kCols; c += 16) {
+        uint32_t v[16];
+        tmem_ld16<false>(lane_addr + accr.s * NT + c, v);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c + i] = __uint_as_float(v[i]);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&acc_empty[accr.s]);
+      accr.next();
+      if (p.ks > 1) {
+        // The slice's sums; the warp that comes last of a (tile, tokens) adds
+        // them up in the order of the slices.
+        float *part = p.partial + ((int64_t)t * p.ks * NT + col0) * kI8PadN + lg * 32 + lane;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i)
+          if (i < cols) __stcg(part + ((int64_t)slice * NT + i) * kI8PadN, acc[i]);
+        __threadfence();
+        __syncwarp();
+        int before = 0;
+        int *counter = p.counters + (int64_t)t * 4 * G::kEpi + 4 * pw + lg;
+        if (lane == 0) before = atomicAdd(counter, 1);
+        before = __shfl_sync(0xffffffffu, before, 0);
+        if (before != p.ks - 1) continue;
+        __threadfence();
+        if (lane == 0) *counter = 0;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+        for (int s = 0; s < p.ks; ++s)
+#pragma unroll
+          for (int i = 0; i < kCols; ++i)
+            if (i < cols) acc[i] += __ldcg(part + ((int64_t)s * NT + i) * kI8PadN);
+      }
+      if (n < p.N) {
+        if (p.out.dtype == ARCHEAD_DTYPE_FP32)
+          store_channel<float>(p.out, m0, n, acc, cols, p.x_scales, sw);
+        else if (p.out.dtype == ARCHEAD_DTYPE_FP16)
+          store_channel<__half>(p.out, m0, n, acc, cols, p.x_scales, sw);
+        else
+          store_channel<__nv_bfloat16>(p.out, m0, n, acc, cols, p.x_scales, sw);
+      }
+    }
+  }
+done:
+  if (warp == 1 && mma_leader) {
+    tc_commit(drain);
+    mbar_wait(drain, 0, p.wait_budget, nullptr, p.err);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kPfTmemCols);
+  }
+}
+
+namespace {
+
+template <int NT>
+cudaError_t launch_gemm_t(const I8GemmParams &p, int grid, cudaStream_t s) {
+  auto kern = int8_gemm_kernel<NT>;
+  cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), I8Geom<NT>::kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(I8Geom<NT>::kThreads);
+  cfg.dynamicSmemBytes = I8Geom<NT>::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+}  // namespace
+
+I8GemmPlan int8_gemm_plan(const archead_int8_weight *w, int64_t M) {
+  I8GemmPlan f;
+  f.NT = M <= 64 ? 64 : M <= 128 ? 128 : 256;
+  const int64_t tiles = w->N_pad / kI8PadN;
+  f.num_mt = (M + f.NT - 1) / f.NT;
+  f.nt = (int)(((M + f.num_mt - 1) / f.num_mt + 15) / 16 * 16);
+  const int64_t pairs = tiles * f.num_mt;
+  const int KC = w->K_pad / kI8PadK;
+  // Too few (tile, tokens) for the multiprocessors: K in slices of at least four stages.
+  f.ks = 1;
+  if (pairs * 2 <= w->sm_count) f.ks = (int)std::max<int64_t>(1, std::min<int64_t>({w->sm_count / pairs, KC / 4, 8}));
+  f.units = pairs * f.ks;
+  if (f.ks > 1) f.partial_bytes = (size_t)f.units * f.NT * kI8PadN * sizeof(float);
+  return f;
+}
+
+cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, const uint16_t *x,
+                             const float *x_scales, int64_t M, I8Out out, float *partial, cudaStream_t s) {
+  I8GemmParams p{};
+  if (!make_tma_map_bf16(&p.tmap_x, x, M, w->K_pad, f.nt)) return cudaErrorInvalidValue;
+  if (f.units > 0x7fffffff - w->sm_count) return cudaErrorInvalidValue;
+  p.codes = w->codes;
+  p.scales = w->scales;
+  p.x_scales = x_scales;
+  p.out = out;
+  p.N = w->N;
+  p.M = (int)M;
+  p.nt = f.nt;
+  p.num_mt = (int)f.num_mt;
+  p.units = (int)f.units;
+  p.KC = w->K_pad / kI8PadK;
+  p.ks = f.ks;
+  p.partial = partial;
+  p.counters = w->counters;
+  p.err = w->err;
+  p.wait_budget = w->wait_budget;
+  const int grid = (int)std::min<int64_t>(f.units, w->sm_count);
+  return f.NT == 64 ? launch_gemm_t<64>(p, grid, s) : f.NT == 128 ? launch_gemm_t<128>(p, grid, s) : launch_gemm_t<256>(p, grid, s);
+}
+
+}  // namespace archead

@@ -10,13 +10,14 @@ namespace archead {
 // ------------------------------------------------------------------------
 // Weight layout (int8.h): one word a thread.
 // ------------------------------------------------------------------------
-__global__ void int8_layout_kernel(const int8_t *__restrict__ src, int64_t N, int K, int KB, int64_t words,
+__global__ void int8_layout_kernel(const int8_t *__restrict__ src, int64_t N, int K, int KC, int64_t words,
                                    uint32_t *__restrict__ dst) {
   for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < words; i += (int64_t)gridDim.x * blockDim.x) {
     const int j = (int)(i & 3), lane = (int)(i >> 2) & 31;
-    const int64_t blk = i >> 7;
-    const int64_t n = blk / KB * kI8Strip + (lane >> 2) + 8 * (j & 1);
-    const int k = (int)(blk % KB) * kI8Block + 8 * (lane & 3) + 4 * (j >> 1);
+    const int block = (int)(i >> 7) & 3, strip = (int)(i >> 9) & 7;
+    const int64_t st = i >> 12;
+    const int64_t n = st / KC * kI8PadN + strip * kI8Strip + (lane >> 2) + 8 * (j & 1);
+    const int k = (int)(st % KC) * kI8PadK + block * kI8Block + 8 * (lane & 3) + 4 * (j >> 1);
     uint32_t w = 0;
     if (n < N) {
 #pragma unroll
@@ -31,7 +32,7 @@ cudaError_t launch_int8_layout(const archead_int8_weight *w, const int8_t *codes
   const int64_t words = w->N_pad * w->K_pad / 4;
   const int64_t blocks = (words + 255) / 256;
   int8_layout_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(
-      codes, w->N, w->K, w->K_pad / kI8Block, words, reinterpret_cast<uint32_t *>(w->codes));
+      codes, w->N, w->K, w->K_pad / kI8PadK, words, reinterpret_cast<uint32_t *>(w->codes));
   return cudaGetLastError();
 }
 
@@ -58,12 +59,12 @@ __global__ void __launch_bounds__(128) int8_product_kernel(const uint4 *__restri
   if (strip * kI8Strip >= N) return;
   const int64_t m0 = (int64_t)blockIdx.y * 8;
   const int KB = K_pad / kI8Block;
-  const uint4 *a = codes + strip * KB * 32 + lane;
+  const uint4 *a = codes + ((strip >> 3) * KB * 8 + (strip & 7) * 4) * 32 + lane;
   const int64_t mb = m0 + gq < M ? m0 + gq : M - 1;  // (columns past M are computed and not stored)
   const int8_t *b = x + mb * K_pad + 8 * cq;
   int d[4] = {0, 0, 0, 0};
   for (int kb = 0; kb < KB; ++kb) {
-    const uint4 w = a[kb * 32];
+    const uint4 w = a[((kb >> 2) * 32 + (kb & 3)) * 32];
     const uint2 v = *reinterpret_cast<const uint2 *>(b + kb * kI8Block);
     asm volatile(
         "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
