@@ -345,26 +345,47 @@ def archead_dequant_residual_sc4(codes, scale_codes, row_scale, group_size: int,
            "archead_dequant_residual_sc4")
 
 
-def _dtype(t) -> int:
-    import torch
+_DTYPES: Dict = {}  # torch's types, filled with the first use
+_raw_stream = None
 
-    codes = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, torch.float16: DTYPE_FP16}
-    if t.dtype not in codes:
-        raise ValueError(f"bf16, fp16 or fp32 is wanted, not {t.dtype}")
-    return codes[t.dtype]
+
+def _dtype(t) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        import torch
+
+        _DTYPES.update({torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, torch.float16: DTYPE_FP16})
+        code = _DTYPES.get(t.dtype)
+        if code is None:
+            raise ValueError(f"bf16, fp16 or fp32 is wanted, not {t.dtype}")
+    return code
+
+
+def _stream_at(stream, t) -> int:
+    """The stream given, or the current one of the tensor's device (looked up without a Stream object, which takes
+    longer than a launch)."""
+    global _raw_stream
+    if stream is not None:
+        return _stream_ptr(stream)
+    if _raw_stream is None:
+        import torch
+
+        _raw_stream = torch._C._cuda_getCurrentRawStream
+    return _raw_stream(t.get_device())
 
 
 def _rows(t, rows: int, cols: int, what: str) -> int:
     """Distance of the rows of a matrix of at least `rows` rows whose `cols` columns lie side by side."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols or (stride[1] != 1 and cols > 1):
         raise ValueError(f"{what}: {rows} rows of {cols} adjacent elements are wanted, "
-                         f"not {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else cols
+                         f"not {tuple(shape)} with strides {stride}")
+    return stride[0] if shape[0] > 1 else cols
 
 
 def _flat(t, dtype, size: int, what: str):
-    """A contiguous tensor of at least `size` elements of the type."""
-    if t.dtype != dtype or t.numel() < size or not t.is_contiguous():
+    """Address of a contiguous tensor of at least `size` elements of the type."""
+    if t.dtype is not dtype or t.numel() < size or not t.is_contiguous():
         raise ValueError(f"{what}: {size} contiguous elements of {dtype} are wanted, not {tuple(t.shape)} of {t.dtype}")
     return t.data_ptr()
 
@@ -426,7 +447,7 @@ def archead_int8_quantize_tokens(x, codes, scales, stream=None) -> None:
     M, K = x.shape
     ldx = _rows(x, M, K, "x")
     _check(load().archead_int8_quantize_tokens(x.data_ptr(), _dtype(x), M, K, ldx, _flat(codes, torch.int8, M * K, "codes"),
-                                               _flat(scales, torch.float32, M, "scales"), _stream_ptr(stream)),
+                                               _flat(scales, torch.float32, M, "scales"), _stream_at(stream, x)),
            "archead_int8_quantize_tokens")
 
 
@@ -441,14 +462,14 @@ def archead_int8_matmul_path(weight: Int8Weight, x_codes, x_scales, M: int, y, p
     ldy = _rows(y, M, weight.N, "y")
     _check(load().archead_int8_matmul_path(weight.handle, _flat(x_codes, torch.int8, M * weight.K, "x_codes"),
                                            _flat(x_scales, torch.float32, M, "x_scales"), M, y.data_ptr(), _dtype(y),
-                                           ldy, path, _stream_ptr(stream)), "archead_int8_matmul")
+                                           ldy, path, _stream_at(stream, y)), "archead_int8_matmul")
 
 
 def archead_int8_linear(weight: Int8Weight, x, M: int, y, stream=None) -> None:
     """y [M, N] of activations x [M, K], which the call quantises (each bf16, fp16 or fp32, rows any distance apart)."""
     ldx, ldy = _rows(x, M, weight.K, "x"), _rows(y, M, weight.N, "y")
     _check(load().archead_int8_linear(weight.handle, x.data_ptr(), _dtype(x), M, ldx, y.data_ptr(), _dtype(y), ldy,
-                                      _stream_ptr(stream)), "archead_int8_linear")
+                                      _stream_at(stream, y)), "archead_int8_linear")
 
 
 def archead_int8_sync_status(weight: Int8Weight, stream=None) -> int:
@@ -507,7 +528,7 @@ def archead_beam_select(beam: Beam, logits, scores, out_scores, out_parents, out
         None if ended is None else _flat(ended, torch.uint8, batch * beams, "ended"), end_token, n,
         _flat(out_scores, torch.float32, batch * n, "out_scores"),
         _flat(out_parents, torch.int32, batch * n, "out_parents"),
-        _flat(out_tokens, torch.int32, batch * n, "out_tokens"), _stream_ptr(stream)), "archead_beam_select")
+        _flat(out_tokens, torch.int32, batch * n, "out_tokens"), _stream_at(stream, logits)), "archead_beam_select")
 
 
 def _merged(shape, strides, what: str):
@@ -595,7 +616,7 @@ def archead_beam_reorder(states: BeamStates, parents, length: int = 0, stream=No
         raise ValueError(f"{batch * beams} rows of {length} positions in states of {states.rows} rows and "
                          f"{states.room} positions")
     _check(load().archead_beam_reorder(states.array, states.count, _flat(parents, torch.int32, batch * beams, "parents"),
-                                       batch, beams, length, _stream_ptr(stream)), "archead_beam_reorder")
+                                       batch, beams, length, _stream_at(stream, parents)), "archead_beam_reorder")
 
 
 def archead_pack_bytes(pack: Pack) -> int:

@@ -16,8 +16,8 @@ struct archead_beam {
 
 namespace archead {
 
-// A row of logits is cut into slices; a slice leaves (max, sum of exp(l - max))
-// and its n best (logit, token) keys, best first.
+// A row of logits is cut into slices (a block each) of segments; a slice leaves
+// (m, sum of exp(l - m)), a segment its largest logit.
 struct SelectParams {
   const void *logits;
   int64_t ld;
@@ -25,18 +25,20 @@ struct SelectParams {
   const float *scores;
   const uint8_t *ended;  // may be NULL
   int32_t end_token;
-  int slices, slice_len;
+  int segments, slices, slice_segments;
+  bool vec;         // rows start on 16 bytes
+  int *counters;    // [batch] blocks that have finished, zero between calls
   float2 *part;     // [rows][slices]
-  uint64_t *keys;   // [rows][slices][n]
+  float *tops;      // [rows][segments]
   float *out_scores;
   int32_t *out_parents, *out_tokens;
 };
 
-// Slices that a selection cuts each row into, and the scratch of the largest one.
-int beam_slices(int64_t rows, int64_t vocab, int sm_count);
-size_t beam_scratch_bytes(int64_t max_rows, int max_out, int sm_count);
+// Scratch of the largest selection; its counters, which come first, start as zeros.
+size_t beam_scratch_bytes(int64_t max_rows, int64_t max_vocab, int sm_count);
+size_t beam_counter_bytes(int64_t max_rows);
 
-cudaError_t launch_beam_select(SelectParams p, int dtype, int64_t batch, void *ws, int sm_count, cudaStream_t s);
+cudaError_t launch_beam_select(SelectParams p, int dtype, void *ws, int64_t max_rows, int sm_count, cudaStream_t s);
 
 constexpr int kReorderStates = 48;  // states of one launch
 struct ReorderState {

@@ -28,10 +28,18 @@ archead_status archead_beam_create(int64_t max_rows, int64_t max_vocab, int max_
   b->max_out = max_out;
   cudaError_t e = cudaGetDevice(&b->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&b->sm_count, cudaDevAttrMultiProcessorCount, b->device);
-  if (e == cudaSuccess) e = cudaMalloc(&b->ws, beam_scratch_bytes(max_rows, max_out, b->sm_count));
+  if (e == cudaSuccess) e = cudaMalloc(&b->ws, beam_scratch_bytes(max_rows, max_vocab, b->sm_count));
+  // (In a stream of its own, waited for: any stream may use the handle first.)
+  cudaStream_t s = nullptr;
+  if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+  if (e == cudaSuccess) e = cudaMemsetAsync(b->ws, 0, beam_counter_bytes(max_rows), s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (s) cudaStreamDestroy(s);
   if (e != cudaSuccess) {
+    const archead_status st = status_of(e);
+    if (b->ws) cudaFree(b->ws);
     delete b;
-    return status_of(e);
+    return st;
   }
   *out = b;
   return ARCHEAD_OK;
@@ -74,7 +82,7 @@ archead_status archead_beam_select(archead_beam *beam, const void *logits, arche
   p.out_scores = out_scores;
   p.out_parents = out_parents;
   p.out_tokens = out_tokens;
-  AH_TRY(launch_beam_select(p, dtype, batch, beam->ws, beam->sm_count, static_cast<cudaStream_t>(stream)));
+  AH_TRY(launch_beam_select(p, dtype, beam->ws, beam->max_rows, beam->sm_count, static_cast<cudaStream_t>(stream)));
   return ARCHEAD_OK;
 }
 

@@ -1,199 +1,623 @@
 // Selection of the next beams: of each batch entry's beams x vocabulary
 // candidates, value = (score - lse) + logit, the n largest (include/archead.h).
 //
-// Two launches.  The first reads the logits once: a block takes a slice of a
-// row and leaves the slice's (max, sum of exp) and its n best logits.  The
-// second, a block for each batch entry, joins the slices' sums into the
-// log-sum-exp of each beam and merges the slices' lists.
+// One launch that reads the logits once and a few of them again; bound by
+// memory, at few rows by latency.  A warp takes segments of 512 logits (16 a
+// lane, copied some segments ahead into shared memory by asynchronous copies
+// that each thread waits for itself) and keeps, without meeting any other, its
+// lanes' sums of exp(l - m) for a reference m near the maximum; each segment
+// leaves its largest logit.  The block that finishes last of a batch entry
+//   - joins the blocks' sums, in their order, into each beam's log-sum-exp;
+//   - finds the n best segments by their largest values: no other holds one of
+//     the n best candidates;
+//   - reads those again and takes the n best candidates of them.
+// Both searches go by a threshold first: of the maxima of G groups of threads
+// the n-th largest is no more than the n-th largest of all, and with G = 4 n it
+// is passed by about 1.15 n.  Candidates compare by value, beam, logit and token
+// (segments by their number), so there are no ties and what passes is bounded.
+//
+// (Keeping a list of the n best in every block cost more than the reading: lists
+// with a threshold that all warps share met at a barrier for every tile, lists
+// of a warp's own let too much pass; 512 rows of 151936 in bf16 took 69 us.)
+//
+// Sums are fp32: each thread's over its logits of the segments in turn, then a
+// fixed tree; a row's depends on its logits alone, so that equal beams tie.
 #include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
 
 #include "beam.h"
 #include "device.cuh"
+#include "internal.h"
 
 namespace archead {
 
 namespace {
 
-constexpr int kThreads = 256;
-
-__device__ __forceinline__ float load_logit(const float *p) { return *p; }
-__device__ __forceinline__ float load_logit(const __half *p) { return __half2float(*p); }
-__device__ __forceinline__ float load_logit(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kE = 16;                     // logits of a lane and segment
+constexpr int kSegment = 32 * kE;
+constexpr int kList = 64 + 1024;           // entries: the best so far, and what passes a threshold of groups
+constexpr float kLog2e = 1.4426950408889634f;
 
 // Key of (logit, token): a larger logit, or the lower token of equal ones, has
 // the larger key.  (Adding 0 makes the two zeros one.)  0 is no candidate.
-__device__ __forceinline__ uint64_t make_key(float l, uint32_t token) {
-  const uint32_t b = __float_as_uint(l + 0.f);
-  return (uint64_t)(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) << 32 | (uint32_t)~token;
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float key_logit(uint64_t key) {
-  const uint32_t o = (uint32_t)(key >> 32);
+__device__ __forceinline__ float unordered(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+__device__ __forceinline__ uint64_t make_key(float l, uint32_t token) {
+  return (uint64_t)ordered(l) << 32 | (uint32_t)~token;
 }
 __device__ __forceinline__ uint32_t key_token(uint64_t key) { return ~(uint32_t)key; }
 
-__device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const uint64_t other = __shfl_xor_sync(0xffffffffu, k, o);
-    k = other > k ? other : k;
-  }
-  return k;
+__device__ __forceinline__ float exp_of(float d) {  // e^d, d <= 0: relative error of a few 2^-23
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(d * kLog2e));
+  return y;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) beam_slice_kernel(SelectParams p) {
-  __shared__ float red[kThreads / 32];
-  __shared__ uint64_t kred[kThreads / 32];
-  const int r = blockIdx.x / p.slices, sl = blockIdx.x % p.slices, t = threadIdx.x;
-  if (p.ended && p.ended[r]) return;
-  const int v0 = sl * p.slice_len, v1 = min(p.vocab, v0 + p.slice_len);
-  const T *row = static_cast<const T *>(p.logits) + (int64_t)r * p.ld;
-  float m = -INFINITY;
-  for (int v = v0 + t; v < v1; v += kThreads) m = fmaxf(m, load_logit(row + v));
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if ((t & 31) == 0) red[t >> 5] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, red[w]);
-  __syncthreads();
-  const float ref = m == -INFINITY ? 0.f : m;
-  float s = 0.f;
-  for (int v = v0 + t; v < v1; v += kThreads) s += expf(load_logit(row + v) - ref);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if ((t & 31) == 0) red[t >> 5] = s;
-  __syncthreads();
-  const int64_t part = (int64_t)r * p.slices + sl;
-  if (t == 0) {
-    s = 0.f;
-    for (int w = 0; w < kThreads / 32; ++w) s += red[w];
-    p.part[part] = make_float2(m, s);
-  }
-  // The n best, one after the other.
-  uint64_t last = ~0ull;
-  for (int i = 0; i < p.n; ++i) {
-    uint64_t best = 0;
-    for (int v = v0 + t; v < v1; v += kThreads) {
-      const float l = load_logit(row + v);
-      const uint64_t k = l > -INFINITY ? make_key(l, v) : 0;
-      if (k < last && k > best) best = k;
+__device__ __forceinline__ float exp2_of(float d) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(d));
+  return y;
+}
+
+// A thread's sum of exp(l - m) for a reference m: a maximum seen before, replaced
+// when a logit passes it by 16 (terms stay below e^16, whose sums fp32 holds as
+// exactly as any).  It is kept as sum of 2^(l log2e - c) with c = m log2e
+// rounded: an FMA rounds only that difference, and what c misses of m log2e is
+// put right where m changes and at the end.  A reference whose c would overflow
+// (rows masked with the type's lowest value), or none yet, takes exp(l - m) as
+// it stands.
+struct RunningSum {
+  float m = -INFINITY, c = 0.f, s = 0.f;
+  __device__ __forceinline__ static bool scaled(float m) { return fabsf(m) < 1e38f; }
+  template <int kN>
+  __device__ __forceinline__ void add(const float (&x)[kN], float top) {
+    if (top > m + 16.f) {
+      s = value();
+      if (m > -INFINITY) s *= exp_of(m - top);
+      m = top;
+      c = m * kLog2e;
+      if (scaled(m)) s *= exp2_of(fmaf(m, kLog2e, -c));
     }
-    best = warp_max_key(best);
-    __syncthreads();
-    if ((t & 31) == 0) kred[t >> 5] = best;
-    __syncthreads();
+    if (scaled(m)) {
+      float2 sum = make_float2(0.f, 0.f);
+      const float2 scale = make_float2(kLog2e, kLog2e), shift = make_float2(-c, -c);
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) best = kred[w] > best ? kred[w] : best;
-    if (t == 0) p.keys[part * p.n + i] = best;
-    last = best;
+      for (int i = 0; i < kN; i += 2) {
+        const float2 d = __ffma2_rn(make_float2(x[i], x[i + 1]), scale, shift);
+        sum = __fadd2_rn(sum, make_float2(exp2_of(d.x), exp2_of(d.y)));
+      }
+      s += sum.x + sum.y;
+    } else {
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) s += exp_of(x[i] - ref);
+    }
+  }
+  // The sum of exp(l - m).
+  __device__ __forceinline__ float value() const { return scaled(m) ? s * exp2_of(-fmaf(m, kLog2e, -c)) : s; }
+};
+
+// A lane's sixteen logits of a segment, as they are stored.
+template <typename T>
+struct Raw {
+  static constexpr int kPer = 16 / sizeof(T);  // of a 16-byte load
+  static constexpr int kLoads = kE / kPer;
+  uint4 r[kLoads];
+  // Place of value i within the segment.
+  static __device__ __forceinline__ int place(int i) { return (i / kPer) * 32 * kPer + lane_id() * kPer + i % kPer; }
+  // The values of load c; tokens from `end` on read as -inf.
+  static __device__ __forceinline__ uint4 some(const T *row, int v, int end) {
+    alignas(16) T t[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) t[j] = v + j < end ? row[v + j] : T(-INFINITY);
+    return *reinterpret_cast<const uint4 *>(t);
+  }
+  __device__ __forceinline__ void load(const T *row, int v0, int end, bool vec) {
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c) {
+      const int v = v0 + place(c * kPer);
+      r[c] = vec && v + kPer <= end ? __ldg(reinterpret_cast<const uint4 *>(row + v)) : some(row, v, end);
+    }
+  }
+  // The same of a row that starts on 16 bytes, through this thread's places (16 bytes of each
+  // 256 threads') of a ring slot.
+  static __device__ __forceinline__ void start(uint32_t slot, const T *row, int v0, int end) {
+    if (v0 + kSegment <= end) {
+      const T *src = row + v0 + place(0);
+#pragma unroll
+      for (int c = 0; c < kLoads; ++c)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(slot + c * kThreads * 16),
+                     "l"(src + c * 32 * kPer)
+                     : "memory");
+    } else {
+#pragma unroll
+      for (int c = 0; c < kLoads; ++c) {
+        const int v = v0 + place(c * kPer);
+        if (v + kPer <= end) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(slot + c * kThreads * 16), "l"(row + v)
+                       : "memory");
+        } else {
+          const uint4 q = some(row, v, end);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(slot + c * kThreads * 16), "r"(q.x), "r"(q.y),
+                       "r"(q.z), "r"(q.w)
+                       : "memory");
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void take(uint32_t slot) {
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n"
+                   : "=r"(r[c].x), "=r"(r[c].y), "=r"(r[c].z), "=r"(r[c].w)
+                   : "r"(slot + c * kThreads * 16)
+                   : "memory");
+  }
+  // The largest value (NaNs left out, unless all are).
+  __device__ __forceinline__ float top(const float (&x)[kE]) const {
+    if constexpr (__is_same(T, __nv_bfloat16)) {
+      __nv_bfloat162 m = *reinterpret_cast<const __nv_bfloat162 *>(&r[0].x);
+#pragma unroll
+      for (int i = 1; i < kE / 2; ++i)
+        m = __hmax2(m, reinterpret_cast<const __nv_bfloat162 *>(&r[i / 4])[i % 4]);
+      return fmaxf(__low2float(m), __high2float(m));
+    } else {
+      float m = x[0];
+#pragma unroll
+      for (int i = 1; i < kE; ++i) m = fmaxf(m, x[i]);
+      return m;
+    }
+  }
+  __device__ __forceinline__ void values(float (&x)[kE]) const {
+#pragma unroll
+    for (int c = 0; c < kLoads; ++c) {
+      const uint32_t u[4] = {r[c].x, r[c].y, r[c].z, r[c].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          x[4 * c + i] = __uint_as_float(u[i]);
+        } else if constexpr (__is_same(T, __nv_bfloat16)) {
+          x[8 * c + 2 * i] = bf16_lo(u[i]), x[8 * c + 2 * i + 1] = bf16_hi(u[i]);
+        } else {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+          x[8 * c + 2 * i] = f.x, x[8 * c + 2 * i + 1] = f.y;
+        }
+      }
+    }
+  }
+};
+
+// Groups of threads whose maxima give a threshold.
+__device__ __forceinline__ int groups_for(int n) { return n <= 16 ? 64 : n <= 32 ? 128 : 256; }
+
+// A candidate, or a segment: value and beam in v; logit and token, or largest
+// logit and number, in k.  The zero is none.
+struct Entry {
+  uint64_t v, k;
+};
+__device__ __forceinline__ bool above(const Entry &a, const Entry &b) { return a.v > b.v || (a.v == b.v && a.k > b.k); }
+__device__ __forceinline__ Entry shfl_xor(const Entry &e, int o) {
+  return {__shfl_xor_sync(0xffffffffu, e.v, o), __shfl_xor_sync(0xffffffffu, e.k, o)};
+}
+__device__ __forceinline__ Entry make_entry(float base, int beam, float logit, uint32_t number) {
+  const float v = base + logit;
+  if (!isfinite(v)) return {0, 0};
+  return {(uint64_t)ordered(v) << 32 | (uint32_t)~beam, make_key(logit, number)};
+}
+
+// The best entries seen, in shared memory.
+struct List {
+  Entry *item;    // [kList]
+  Entry *groups;  // [256]
+  Entry *mark;    // the n-th of the groups
+  int *count;
+  int n;
+
+  __device__ __forceinline__ int push(Entry key) {
+    const int at = atomicAdd(count, 1);
+    if (at < kList) item[at] = key;
+    return at;
+  }
+
+  // The n-th largest of the groups' maxima, from each thread's maximum.  A
+  // group's threads share the work of its rank.
+  __device__ Entry nth_of_groups(Entry mine) {
+    const int t = threadIdx.x, G = groups_for(n), per = kThreads / G;
+    for (int o = 1; o < per; o *= 2) {
+      const Entry other = shfl_xor(mine, o);
+      if (above(other, mine)) mine = other;
+    }
+    const int g = t / per;
+    if (t % per == 0) groups[g] = mine;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 8
+    for (int i = t % per; i < G; i += per) {
+      const Entry other = groups[i];
+      rank += above(other, mine) || (i < g && !above(mine, other));
+    }
+    for (int o = 1; o < per; o *= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+    if (rank == n - 1 && t % per == 0) *mark = mine;
+    __syncthreads();
+    return *mark;
+  }
+
+  // Orders the list's n best at its start; what is left of it is dropped.
+  // Returns the n-th (or none: the zero) as the threshold.
+  __device__ Entry tighten() {
+    const int t = threadIdx.x;
+    __syncthreads();
+    int len = min(*count, kList);
+    while (len > max(64, 2 * n)) {
+      // First drop what a threshold from its own groups of threads excludes.
+      constexpr int kMost = (kList + kThreads - 1) / kThreads;
+      Entry mine[kMost], best = {0, 0};
+#pragma unroll
+      for (int j = 0; j < kMost; ++j) {
+        mine[j] = t + j * kThreads < len ? item[t + j * kThreads] : Entry{0, 0};
+        if (above(mine[j], best)) best = mine[j];
+      }
+      const Entry least = nth_of_groups(best);
+      if (t == 0) *count = 0;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kMost; ++j)
+        if (t + j * kThreads < len && !above(least, mine[j])) push(mine[j]);
+      __syncthreads();
+      const int now = *count;
+      if (now == len) break;  // (nothing to drop)
+      __syncthreads();
+      len = now;
+    }
+    if (len <= kThreads) {
+      // 256, 128 or 64 entries: 1, 2 or 4 threads an entry.
+      const int per = len <= 64 ? 4 : len <= 128 ? 2 : 1, e = t / per;
+      Entry mine{};
+      int rank = 0;
+      if (e < len) {
+        mine = item[e];
+#pragma unroll 8
+        for (int i = t % per; i < len; i += per) rank += above(item[i], mine);
+      }
+      for (int o = 1; o < per; o *= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+      __syncthreads();
+      if (e < len && t % per == 0 && rank < n) item[rank] = mine;
+    } else {
+      // (as many as no threshold of groups could drop)
+      constexpr int kMost = (kList + kThreads - 1) / kThreads;
+      Entry mine[kMost];
+      int rank[kMost];
+#pragma unroll
+      for (int j = 0; j < kMost; ++j) {
+        rank[j] = 0;
+        mine[j] = t + j * kThreads < len ? item[t + j * kThreads] : Entry{0, 0};
+        if (t + j * kThreads < len)
+          for (int i = 0; i < len; ++i) rank[j] += above(item[i], mine[j]);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kMost; ++j)
+        if (t + j * kThreads < len && rank[j] < n) item[rank[j]] = mine[j];
+    }
+    if (t == 0) *count = min(len, n);
+    __syncthreads();
+    return len >= n ? item[n - 1] : Entry{0, 0};
+  }
+};
+
+__device__ __forceinline__ float warp_max_f(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_sum_f(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Segments under way ahead of the one at work.
+template <typename T>
+constexpr int kAhead = sizeof(T) == 4 ? 2 : 3;
+template <typename T>
+constexpr int kRing = (kAhead<T> + 1) * kThreads * kE * (int)sizeof(T);
+
+// A block's share of a row: the segments' largest logits, and (m, sum).
+template <typename T>
+__device__ void reduce_slice(const SelectParams &p, int r, int sl, uint4 *ring, float *red) {
+  constexpr uint32_t kSlot = kThreads * Raw<T>::kLoads * 16;
+  const uint32_t ring0 = smem_u32(ring) + 16 * threadIdx.x, ring1 = ring0 + kRing<T>;
+  const int warp = threadIdx.x >> 5, lane = lane_id();
+  const int s1 = min(p.segments, (sl + 1) * p.slice_segments);
+  const T *row = static_cast<const T *>(p.logits) + (int64_t)r * p.ld;
+  float *tops = p.tops + (int64_t)r * p.segments;
+  RunningSum sum;
+  int next = sl * p.slice_segments + warp;
+  uint32_t in = ring0, out = ring0;
+  const auto start = [&] {
+    if (p.vec && next < s1) Raw<T>::start(in, row, next * kSegment, p.vocab);
+    next += kWarps;
+    in = in + kSlot == ring1 ? ring0 : in + kSlot;
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead<T>; ++i) start();
+  for (int s = sl * p.slice_segments + warp; s < s1; s += kWarps) {
+    start();
+    Raw<T> raw;
+    if (p.vec) {
+      asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead<T>) : "memory");
+      raw.take(out);
+    } else {
+      raw.load(row, s * kSegment, p.vocab, false);
+    }
+    out = out + kSlot == ring1 ? ring0 : out + kSlot;
+    float x[kE];
+    raw.values(x);
+    const float top = raw.top(x);
+    const uint32_t most = __reduce_max_sync(0xffffffffu, top >= -INFINITY ? ordered(top) : 0);  // (a NaN: none)
+    if (lane == 0) tops[s] = most ? unordered(most) : -INFINITY;
+    sum.add(x, top);
+  }
+  asm volatile("cp.async.wait_all;\n" ::: "memory");
+  // The threads' sums, to the block's reference.
+  const float m = sum.m, wm = warp_max_f(m);
+  if (lane == 0) red[warp] = wm;
+  __syncthreads();
+  float all = red[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) all = fmaxf(all, red[w]);
+  const float ws = warp_sum_f(sum.value() * exp_of(m - (all == -INFINITY ? 0.f : all)));
+  if (lane == 0) red[kWarps + warp] = ws;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) s += red[kWarps + w];
+    p.part[(int64_t)r * p.slices + sl] = make_float2(all, s);
   }
 }
 
-// A candidate in the order of the result: value, then beam, then its key.
-struct Cand {
-  float v;
-  int beam;
-  uint64_t key;
-};
-__device__ __forceinline__ bool before(const Cand &a, const Cand &b) {
-  if (a.v != b.v) return a.v > b.v;
-  if (a.beam != b.beam) return a.beam < b.beam;
-  return a.key > b.key;
-}
-
-__global__ void __launch_bounds__(kThreads) beam_merge_kernel(SelectParams p) {
-  extern __shared__ int smem[];
-  int *head = smem;                                          // [beams * slices]
-  float *base = reinterpret_cast<float *>(head + p.beams * p.slices);  // [beams]
-  __shared__ Cand red[kThreads / 32];
-  const int b = blockIdx.x, t = threadIdx.x;
-  const int lists = p.beams * p.slices;
-  for (int i = t; i < lists; i += kThreads) head[i] = 0;
-  for (int k = t; k < p.beams; k += kThreads) {
-    const int r = b * p.beams + k;
-    const float score = p.scores[r];
-    if (p.ended && p.ended[r]) {
-      base[k] = score;
+// The n best candidates of a batch entry.
+template <typename T>
+__device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segments, float *base) {
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31, r0 = b * p.beams;
+  const float *tops = p.tops + (int64_t)r0 * p.segments;
+  const int all = p.beams * p.segments;
+  constexpr int kU = 6;  // segments of a thread at once
+  float top[kU];
+  const auto load_tops = [&](int at) {
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int i = at + t + j * kThreads;
+      top[j] = i < all ? __ldcg(tops + i) : -INFINITY;
+    }
+  };
+  load_tops(0);
+  for (int k = warp; k < p.beams; k += kWarps) {  // a warp a beam
+    const float score = p.scores[r0 + k];
+    if (p.ended && p.ended[r0 + k]) {
+      if (lane == 0) base[k] = score;
       continue;
     }
-    const float2 *part = p.part + (int64_t)r * p.slices;
-    float m = -INFINITY, s = 0.f;
-    for (int i = 0; i < p.slices; ++i) m = fmaxf(m, part[i].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    for (int i = 0; i < p.slices; ++i) s += part[i].y * expf(part[i].x - ref);
-    base[k] = score - (m + logf(s));
+    const float2 *part = p.part + (int64_t)(r0 + k) * p.slices;
+    float m = -INFINITY, s = 0.f;  // a lane's blocks, in turn
+    for (int i = lane; i < p.slices; i += 32) {
+      const float2 q = __ldcg(part + i);
+      const float now = fmaxf(m, q.x), ref = now == -INFINITY ? 0.f : now;
+      s = s * exp_of(m - ref) + q.y * exp_of(q.x - ref);
+      m = now;
+    }
+    const float most = warp_max_f(m);
+    s = warp_sum_f(s * exp_of(m - (most == -INFINITY ? 0.f : most)));
+    if (lane == 0) base[k] = score - (most + logf(s));
+  }
+  if (t == 0) *list.count = 0;
+  __syncthreads();
+
+  // Segment i % segments of beam i / segments; an ended beam is one segment, whose logit is 0.
+  const float per = 1.f / (float)p.segments;
+  const auto segment = [&](int i, float l) -> Entry {
+    if (i >= all) return {0, 0};
+    int k = (int)(((float)i + 0.5f) * per);  // (one off at most)
+    k -= k * p.segments > i;
+    k += (k + 1) * p.segments <= i;
+    const int s = i - k * p.segments;
+    if (p.ended && p.ended[r0 + k]) return s == 0 ? make_entry(base[k], k, 0.f, 0) : Entry{0, 0};
+    return make_entry(base[k], k, l, s);
+  };
+  Entry best = {0, 0}, mine[kU];
+  for (int at = 0; at < all; at += kU * kThreads) {
+    if (at > 0) load_tops(at);
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      mine[j] = segment(at + t + j * kThreads, top[j]);
+      if (above(mine[j], best)) best = mine[j];
+    }
+  }
+  Entry least = list.nth_of_groups(best);
+  while (true) {
+    for (int at = 0; at < all; at += kU * kThreads) {
+      if (all > kU * kThreads) {
+        load_tops(at);
+#pragma unroll
+        for (int j = 0; j < kU; ++j) mine[j] = segment(at + t + j * kThreads, top[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < kU; ++j)
+        if (mine[j].v && !above(least, mine[j])) list.push(mine[j]);
+    }
+    __syncthreads();
+    const bool over = *list.count > kList;
+    const Entry nth = list.tighten();
+    if (above(nth, least)) least = nth;
+    if (!over) break;
+    // More than the list takes: the n-th of those it took is a higher threshold.
+    if (t == 0) *list.count = 0;
+    __syncthreads();
+  }
+
+  // The candidates of those segments.
+  const int chosen = *list.count;
+  if (t < chosen) best_segments[t] = list.item[t];
+  __syncthreads();
+  if (t == 0) *list.count = 0;
+  __syncthreads();
+  // (As a candidate's, the threshold's token is the last of its segment.)
+  least.k = (least.k & ~0xFFFFFFFFull) | (uint32_t)~((key_token(least.k) + 1) * kSegment - 1);
+  // This lane's logits of the c-th segment, of beam k and from token v (an ended beam: a logit of 0 in place 0).
+  const auto load_segment = [&](int c, float(&x)[kE], int &k, int &v) {
+#pragma unroll
+    for (int i = 0; i < kE; ++i) x[i] = -INFINITY;
+    k = v = 0;
+    if (c >= chosen) return;
+    const Entry seg = best_segments[c];
+    k = (int)~(uint32_t)seg.v;
+    if (p.ended && p.ended[r0 + k]) {
+      if (lane == 0) x[0] = 0.f;
+    } else {
+      v = (int)key_token(seg.k) * kSegment;
+      Raw<T> raw;
+      raw.load(static_cast<const T *>(p.logits) + (int64_t)(r0 + k) * p.ld, v, p.vocab, p.vec);
+      raw.values(x);
+    }
+  };
+  // The candidates that reach the threshold, straight away: about as many as there are segments.
+  const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
+  for (int c = warp; c < chosen; c += kWarps) {
+    float x[kE];
+    int k, v;
+    load_segment(c, x, k, v);
+    const float plus = base[k];
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (plus + x[i] >= bar) {
+        const Entry e = make_entry(plus, k, x[i], v + Raw<T>::place(i));
+        if (e.v && !above(least, e)) list.push(e);
+      }
   }
   __syncthreads();
-  for (int i = 0; i < p.n; ++i) {
-    Cand best = {-INFINITY, p.beams, 0};
-    int from = -1;
-    for (int j = t; j < lists; j += kThreads) {
-      const int k = j / p.slices, r = b * p.beams + k;
-      Cand c = {-INFINITY, k, 0};
-      if (p.ended && p.ended[r]) {
-        if (j % p.slices == 0 && head[j] == 0) c.v = base[k], c.key = ~(uint64_t)(uint32_t)p.end_token;
-      } else if (head[j] < p.n) {
-        c.key = p.keys[((int64_t)r * p.slices + j % p.slices) * p.n + head[j]];
-        if (c.key) c.v = base[k] + key_logit(c.key);
+  if (*list.count > kList) {
+    // More than the list takes (a segment that holds many of the best): again,
+    // eight segments, one a warp, at a time, with a threshold that rises.
+    __syncthreads();
+    if (t == 0) *list.count = 0;
+    for (int c = 0; c < chosen; c += kWarps) {
+      float x[kE];
+      int k, v;
+      load_segment(c + warp, x, k, v);
+      const float plus = base[k];
+      Entry top_entry = {0, 0};
+#pragma unroll
+      for (int i = 0; i < kE; ++i) {
+        const Entry e = make_entry(plus, k, x[i], v + Raw<T>::place(i));
+        if (above(e, top_entry)) top_entry = e;
       }
-      if (!isfinite(c.v)) continue;
-      if (from < 0 || before(c, best)) best = c, from = j;
-    }
-    Cand mine = best;
+      // (At most n groups' 16 * 256 / G candidates reach it: 1024.)
+      const Entry mark = list.nth_of_groups(top_entry);
+      if (above(mark, least)) least = mark;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      Cand other;
-      other.v = __shfl_xor_sync(0xffffffffu, best.v, o);
-      other.beam = __shfl_xor_sync(0xffffffffu, best.beam, o);
-      other.key = __shfl_xor_sync(0xffffffffu, best.key, o);
-      if (before(other, best)) best = other;
+      for (int i = 0; i < kE; ++i) {
+        const Entry e = make_entry(plus, k, x[i], v + Raw<T>::place(i));
+        if (e.v && !above(least, e)) list.push(e);
+      }
+      const Entry nth = list.tighten();
+      if (above(nth, least)) least = nth;
     }
-    if ((t & 31) == 0) red[t >> 5] = best;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w)
-      if (before(red[w], best)) best = red[w];
-    if (from >= 0 && mine.beam == best.beam && mine.key == best.key) ++head[from];
-    if (t == 0) {
-      const bool none = best.v == -INFINITY;
-      const int64_t o = (int64_t)b * p.n + i;
-      p.out_scores[o] = best.v;
-      p.out_parents[o] = none ? -1 : best.beam;
-      p.out_tokens[o] = none ? -1 : (int32_t)key_token(best.key);
-    }
-    __syncthreads();
+  } else {
+    list.tighten();
   }
+  const int len = *list.count;
+  for (int i = t; i < p.n; i += kThreads) {
+    const int64_t o = (int64_t)b * p.n + i;
+    const bool there = i < len;
+    const Entry e = there ? list.item[i] : Entry{0, 0};
+    p.out_scores[o] = there ? unordered((uint32_t)(e.v >> 32)) : -INFINITY;
+    const int k = there ? (int)~(uint32_t)e.v : -1;
+    p.out_parents[o] = k;
+    p.out_tokens[o] = !there ? -1 : p.ended && p.ended[r0 + k] ? p.end_token : (int32_t)key_token(e.k);
+  }
+}
+
+static_assert(kRing<__half> >= kList * (int)sizeof(Entry), "the list takes the ring's place");
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_kernel(const SelectParams p) {
+  extern __shared__ uint4 smem16[];
+  __shared__ Entry groups[256], mark, best_segments[ARCHEAD_BEAM_MAX_OUT];
+  __shared__ float red[ARCHEAD_BEAM_MAX_BEAMS];
+  __shared__ int count, before;
+  const int r = blockIdx.x / p.slices, sl = blockIdx.x - r * p.slices, b = r / p.beams;
+  if (!(p.ended && p.ended[r])) reduce_slice<T>(p, r, sl, smem16, red);
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) before = atomicAdd(p.counters + b, 1);
+  __syncthreads();
+  if (before != p.beams * p.slices - 1) return;
+  __threadfence();
+  if (threadIdx.x == 0) p.counters[b] = 0;
+  List list = {reinterpret_cast<Entry *>(smem16), groups, &mark, &count, p.n};
+  merge<T>(p, b, list, best_segments, red);
 }
 
 }  // namespace
 
-int beam_slices(int64_t rows, int64_t vocab, int sm_count) {
-  const int64_t want = (4 * sm_count + rows - 1) / rows, most = (vocab + 1023) / 1024;
-  return (int)(want < most ? want : most);
+// Blocks of a row: the least work on the busiest multiprocessor, where a block's
+// start and end cost as much as eight segments, and fewer than three blocks at
+// once leave it waiting for memory.
+static int beam_slices(int64_t rows, int64_t segments, int sm_count) {
+  const int64_t most = std::min<int64_t>((segments + kWarps - 1) / kWarps, 1 + 8 * sm_count / rows);
+  int best = 1;
+  double least = 1e30;
+  for (int64_t n = 1; n <= most; ++n) {
+    const double blocks = (double)(rows * n) / sm_count;
+    const double cost = std::ceil(blocks) * ((double)segments / n / kWarps + 1) * std::max(1.0, 3 / blocks);
+    if (cost < least) {
+      least = cost;
+      best = (int)n;
+    }
+  }
+  return best;
 }
 
-size_t beam_scratch_bytes(int64_t max_rows, int max_out, int sm_count) {
-  return (size_t)(max_rows + 4 * sm_count) * (sizeof(float2) + max_out * sizeof(uint64_t)) + 512;
+// Scratch: counters of the batch entries (at most one a row), the blocks' sums, the segments' largest logits.
+static size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
+size_t beam_counter_bytes(int64_t max_rows) { return up((size_t)max_rows * sizeof(int)); }
+size_t beam_scratch_bytes(int64_t max_rows, int64_t max_vocab, int sm_count) {
+  const size_t segments = (size_t)((max_vocab + kSegment - 1) / kSegment);
+  return beam_counter_bytes(max_rows) + up((size_t)(max_rows + 8 * sm_count) * sizeof(float2)) +
+         (size_t)max_rows * segments * sizeof(float);
 }
 
-cudaError_t launch_beam_select(SelectParams p, int dtype, int64_t batch, void *ws, int sm_count, cudaStream_t s) {
-  p.slices = beam_slices(p.rows, p.vocab, sm_count);
-  p.slice_len = (p.vocab + p.slices - 1) / p.slices;
-  p.part = static_cast<float2 *>(ws);
-  p.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + ((size_t)p.rows * p.slices * sizeof(float2) + 255) / 256 * 256);
+cudaError_t launch_beam_select(SelectParams p, int dtype, void *ws, int64_t max_rows, int sm_count, cudaStream_t s) {
+  p.segments = (p.vocab + kSegment - 1) / kSegment;
+  p.slices = beam_slices(p.rows, p.segments, sm_count);
+  p.slice_segments = (p.segments + p.slices - 1) / p.slices;
+  char *at = static_cast<char *>(ws);
+  p.counters = reinterpret_cast<int *>(at);
+  at += beam_counter_bytes(max_rows);
+  p.part = reinterpret_cast<float2 *>(at);
+  p.tops = reinterpret_cast<float *>(at + up((size_t)p.rows * p.slices * sizeof(float2)));
+  const int size = dtype == ARCHEAD_DTYPE_FP32 ? 4 : 2;
+  p.vec = (reinterpret_cast<uintptr_t>(p.logits) & 15) == 0 && p.ld * size % 16 == 0;
   const unsigned grid = (unsigned)p.rows * p.slices;
-  if (dtype == ARCHEAD_DTYPE_FP32)
-    beam_slice_kernel<float><<<grid, kThreads, 0, s>>>(p);
-  else if (dtype == ARCHEAD_DTYPE_FP16)
-    beam_slice_kernel<__half><<<grid, kThreads, 0, s>>>(p);
-  else
-    beam_slice_kernel<__nv_bfloat16><<<grid, kThreads, 0, s>>>(p);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  beam_merge_kernel<<<(unsigned)batch, kThreads, (p.beams * p.slices + p.beams) * 4, s>>>(p);
-  return cudaGetLastError();
+  const auto run = [&](auto kern, int smem) {
+    cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), smem);
+    if (e != cudaSuccess) return e;
+    kern<<<grid, kThreads, smem, s>>>(p);
+    return cudaGetLastError();
+  };
+  return dtype == ARCHEAD_DTYPE_FP32   ? run(beam_select_kernel<float>, kRing<float>)
+         : dtype == ARCHEAD_DTYPE_FP16 ? run(beam_select_kernel<__half>, kRing<__half>)
+                                       : run(beam_select_kernel<__nv_bfloat16>, kRing<__nv_bfloat16>);
 }
 
 }  // namespace archead

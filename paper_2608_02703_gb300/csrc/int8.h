@@ -66,9 +66,17 @@ cudaError_t launch_int8_quantize(const void *x, int dtype, int64_t M, int64_t K,
                                  int64_t ldc, int64_t k_fill, float *scales, cudaStream_t s);
 // Token codes [M][K] into rows of K_pad codes (wide: widened), zero beyond K.
 cudaError_t launch_int8_pad(const int8_t *codes, int64_t M, int K, int K_pad, void *out, bool wide, cudaStream_t s);
-// Product of padded token codes with the weight.
-cudaError_t launch_int8_product(const archead_int8_weight *w, const int8_t *x, const float *x_scales, int64_t M,
-                                I8Out out, cudaStream_t s);
+// Warp-level kernel.  The tokens are activations of type `dtype`, which it
+// quantises (x_scales NULL; int8_decode_quantizes), or codes; rows ldx elements
+// apart.  More tokens than fit take more launches.  If not even
+// eight tokens' codes fit into shared memory, the codes have to be padded rows.
+cudaError_t launch_int8_decode(const archead_int8_weight *w, const void *x, int dtype, int64_t ldx,
+                               const float *x_scales, int64_t M, I8Out out, cudaStream_t s);
+// Most activations that every block quantises for itself (4 tokens of 4096:
+// 7.9 us for 4096 channels, 8.8 with a launch of its own; 8 tokens: 11.4 and 8.8).
+constexpr int64_t kI8FusedQuantize = 16384;
+bool int8_decode_quantizes(int64_t M, int K, int K_pad);
+bool int8_decode_fits(int64_t M, int K_pad);  // all M tokens in one launch
 
 // Tensor-memory kernel: how a product of M tokens is cut.
 struct I8GemmPlan {

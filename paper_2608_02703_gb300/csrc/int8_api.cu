@@ -16,7 +16,7 @@ constexpr int kReserveTokens = 64;  // a new weight's workspace
 
 // A call's kernel and its place in the workspace.
 struct Plan {
-  bool gemm = false;
+  bool gemm = false, direct = false;
   I8GemmPlan g;
   size_t x_off = 0, scale_off = 0, partial_off = 0, total = 0;
 };
@@ -27,14 +27,26 @@ size_t take(size_t &off, size_t bytes) {
   return o;
 }
 
-// AUTO: the warp-level kernel up to 16 tokens, the tensor-memory kernel above.
-constexpr int kDecodeTokens = 16;
+// AUTO takes the warp-level kernel up to 8 tokens, and up to 16 or 32 where the
+// weight is small: there each further eight tokens cost its integer MMAs as
+// much again, the tensor-memory kernel costs its start (measured: DESIGN notes
+// beside the kernels).
+bool auto_decodes(const archead_int8_weight *w, int64_t M) {
+  const int64_t size = w->N_pad * w->K_pad;
+  return M <= 8 || (int8_decode_fits(M, w->K_pad) &&
+                    ((M <= 16 && size <= (int64_t)64 << 20) || (M <= 32 && size <= (int64_t)16 << 20)));
+}
 
-Plan plan(const archead_int8_weight *w, int64_t M, archead_path path) {
+// What a call is given: activations, or codes.
+enum Given { kActivations, kCodes };
+
+Plan plan(const archead_int8_weight *w, int64_t M, Given given, archead_path path) {
   Plan p;
-  p.gemm = path == ARCHEAD_PATH_PREFILL || (path == ARCHEAD_PATH_AUTO && M > kDecodeTokens);
-  p.x_off = take(p.total, (size_t)M * w->K_pad * (p.gemm ? 2 : 1));
-  p.scale_off = take(p.total, (size_t)M * sizeof(float));
+  p.gemm = path == ARCHEAD_PATH_PREFILL || (path == ARCHEAD_PATH_AUTO && !auto_decodes(w, M));
+  // The warp-level kernel takes what it is given where it can.
+  p.direct = !p.gemm && (given == kActivations ? int8_decode_quantizes(M, w->K, w->K_pad) : int8_decode_fits(1, w->K_pad));
+  if (!p.direct) p.x_off = take(p.total, (size_t)M * w->K_pad * (p.gemm ? 2 : 1));
+  if (!p.direct && given == kActivations) p.scale_off = take(p.total, (size_t)M * sizeof(float));
   if (p.gemm) {
     p.g = int8_gemm_plan(w, M);
     p.partial_off = take(p.total, p.g.partial_bytes);
@@ -47,8 +59,8 @@ Plan plan(const archead_int8_weight *w, int64_t M, archead_path path) {
 size_t room_for(const archead_int8_weight *w, int64_t M) {
   size_t most = 0;
   for (int64_t m : {(int64_t)16, (int64_t)32, (int64_t)48, (int64_t)64, (int64_t)128, (int64_t)256, (int64_t)512, (int64_t)1024})
-    if (m < M) most = std::max(most, plan(w, m, ARCHEAD_PATH_AUTO).total);
-  return std::max(most, plan(w, M, ARCHEAD_PATH_AUTO).total);
+    if (m < M) most = std::max(most, plan(w, m, kActivations, ARCHEAD_PATH_AUTO).total);
+  return std::max(most, plan(w, M, kActivations, ARCHEAD_PATH_AUTO).total);
 }
 
 // Growing synchronises the device: a call made earlier on another stream may
@@ -97,7 +109,7 @@ archead_status run_product(archead_int8_weight *w, const Plan &p, const float *x
                            cudaStream_t s) {
   if (p.gemm)
     return status_of(launch_int8_gemm(w, p.g, at<uint16_t>(w, p.x_off), x_scales, M, out, at<float>(w, p.partial_off), s));
-  return status_of(launch_int8_product(w, at<int8_t>(w, p.x_off), x_scales, M, out, s));
+  return status_of(launch_int8_decode(w, at<int8_t>(w, p.x_off), 0, w->K_pad, x_scales, M, out, s));
 }
 
 void free_weight(archead_int8_weight *w) {
@@ -207,7 +219,8 @@ archead_status archead_int8_matmul_path(archead_int8_weight *w, const int8_t *x_
     return ARCHEAD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_TRY(cudaSetDevice(w->device));
-  const Plan p = plan(w, M, path);
+  const Plan p = plan(w, M, kCodes, path);
+  if (p.direct) return status_of(launch_int8_decode(w, x_codes, 0, w->K, x_scales, M, {y, ldy, out_dtype}, s));
   if ((st = ensure_workspace(w, p.total, M, s)) != ARCHEAD_OK) return st;
   AH_TRY(launch_int8_pad(x_codes, M, w->K, w->K_pad, at<void>(w, p.x_off), p.gemm, s));
   return run_product(w, p, x_scales, M, {y, ldy, out_dtype}, s);
@@ -226,7 +239,8 @@ archead_status archead_int8_linear(archead_int8_weight *w, const void *x, archea
   if (M == 0) return ARCHEAD_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_TRY(cudaSetDevice(w->device));
-  const Plan p = plan(w, M, ARCHEAD_PATH_AUTO);
+  const Plan p = plan(w, M, kActivations, ARCHEAD_PATH_AUTO);
+  if (p.direct) return status_of(launch_int8_decode(w, x, x_dtype, ldx, nullptr, M, {y, ldy, out_dtype}, s));
   if ((st = ensure_workspace(w, p.total, M, s)) != ARCHEAD_OK) return st;
   float *scales = at<float>(w, p.scale_off);
   AH_TRY(launch_int8_quantize(x, x_dtype, M, w->K, ldx, at<void>(w, p.x_off), p.gemm, w->K_pad, w->K_pad, scales, s));

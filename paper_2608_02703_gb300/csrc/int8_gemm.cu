@@ -21,7 +21,7 @@
 
 #include <algorithm>
 
-#include "int8.h"
+#include "int8_quant.cuh"
 #include "prefill_kernel.cuh"  // tcgen05 wrappers, ring positions
 
 namespace archead {
@@ -85,23 +85,19 @@ __device__ __forceinline__ void widen_int8x4(uint32_t w, uint32_t &lo, uint32_t 
   hi = *reinterpret_cast<const uint32_t *>(&rb);
 }
 
-template <typename T>
-__device__ __forceinline__ T from_f32(float v);
-template <>
-__device__ __forceinline__ float from_f32<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
-// One channel's sums of kCols tokens, of which `cols` are there.
+// One channel's sums of kCols tokens, of which `cols` are there.  xs: the
+// tokens' scales, token 32 c + lane in xs[c].  (Loaded by every thread where
+// they were used, a load waited for the store before it, which may have been
+// to the same place: 256 tokens of 4096 x 512 took 13 us, now TODO.)
 template <typename T, int kCols>
-__device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_t n, const float (&acc)[kCols], int cols,
-                                              const float *x_scales, float sw) {
+__device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_t n, bool there, const float (&acc)[kCols],
+                                              int cols, const float (&xs)[kCols / 32], float sw) {
   T *y = static_cast<T *>(o.y) + m0 * o.ld + n;
 #pragma unroll
-  for (int i = 0; i < kCols; ++i, y += o.ld)
-    if (i < cols) *y = from_f32<T>(acc[i] * x_scales[m0 + i] * sw);
+  for (int i = 0; i < kCols; ++i, y += o.ld) {
+    const float s = __shfl_sync(0xffffffffu, xs[i / 32], i % 32);
+    if (there && i < cols) *y = from_f32<T>(acc[i] * s * sw);
+  }
 }
 
 template <int NT>
@@ -291,6 +287,9 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
       const int mu = t % p.num_mt * p.nt;
       const int m0 = mu + col0, cols = min(kCols, min(p.M, mu + p.nt) - m0);  // (may be negative: none)
       const float sw = p.scales[n];
+      float xs[kCols / 32];
+#pragma unroll
+      for (int c = 0; c < kCols / 32; ++c) xs[c] = 32 * c + lane < cols ? p.x_scales[m0 + 32 * c + lane] : 0.f;
       if (!mbar_wait_warp(&acc_full[accr.s], accr.ph, p.wait_budget, abort_flag, p.err)) goto done;
       tc_fence_after();
       float acc[kCols];
@@ -329,14 +328,13 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
           for (int i = 0; i < kCols; ++i)
             if (i < cols) acc[i] += __ldcg(part + ((int64_t)s * NT + i) * kI8PadN);
       }
-      if (n < p.N) {
-        if (p.out.dtype == ARCHEAD_DTYPE_FP32)
-          store_channel<float>(p.out, m0, n, acc, cols, p.x_scales, sw);
-        else if (p.out.dtype == ARCHEAD_DTYPE_FP16)
-          store_channel<__half>(p.out, m0, n, acc, cols, p.x_scales, sw);
-        else
-          store_channel<__nv_bfloat16>(p.out, m0, n, acc, cols, p.x_scales, sw);
-      }
+      const bool there = n < p.N;
+      if (p.out.dtype == ARCHEAD_DTYPE_FP32)
+        store_channel<float>(p.out, m0, n, there, acc, cols, xs, sw);
+      else if (p.out.dtype == ARCHEAD_DTYPE_FP16)
+        store_channel<__half>(p.out, m0, n, there, acc, cols, xs, sw);
+      else
+        store_channel<__nv_bfloat16>(p.out, m0, n, there, acc, cols, xs, sw);
     }
   }
 done:
