@@ -207,10 +207,12 @@ __device__ __forceinline__ bool above(const Entry &a, const Entry &b) { return a
 __device__ __forceinline__ Entry shfl_xor(const Entry &e, int o) {
   return {__shfl_xor_sync(0xffffffffu, e.v, o), __shfl_xor_sync(0xffffffffu, e.k, o)};
 }
-__device__ __forceinline__ Entry make_entry(float base, int beam, float logit, uint32_t number) {
-  const float v = base + logit;
+__device__ __forceinline__ Entry entry_of(float v, int beam, float logit, uint32_t number) {
   if (!isfinite(v)) return {0, 0};
   return {(uint64_t)ordered(v) << 32 | (uint32_t)~beam, make_key(logit, number)};
+}
+__device__ __forceinline__ Entry make_entry(float base, int beam, float logit, uint32_t number) {
+  return entry_of(base + logit, beam, logit, number);
 }
 
 // The best entries seen, in shared memory.
@@ -388,72 +390,91 @@ __device__ void reduce_slice(const SelectParams &p, int r, int sl, uint4 *ring, 
 
 // The n best candidates of a batch entry.
 template <typename T>
-__device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segments, float *base) {
+__device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segments, float *base, bool *ended) {
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31, r0 = b * p.beams;
   const float *tops = p.tops + (int64_t)r0 * p.segments;
-  const int all = p.beams * p.segments;
-  constexpr int kU = 6;  // segments of a thread at once
-  float top[kU];
-  const auto load_tops = [&](int at) {
+  // A warp looks at 128 segments of a beam at a time (a job), four a lane, the
+  // next job's loads under way.
+  constexpr int kU = 4;
+  const int per_beam = (p.segments + 32 * kU - 1) / (32 * kU), jobs = p.beams * per_beam;
+  float next[kU], top[kU];
+  int k = 0, s0 = 0;  // of the job at work: beam, this lane's first segment
+  const auto load_job = [&](int job) {
+    const int beam = job / per_beam, s = (job - beam * per_beam) * 32 * kU + lane;
 #pragma unroll
-    for (int j = 0; j < kU; ++j) {
-      const int i = at + t + j * kThreads;
-      top[j] = i < all ? __ldcg(tops + i) : -INFINITY;
+    for (int j = 0; j < kU; ++j)
+      next[j] = job < jobs && s + 32 * j < p.segments ? __ldcg(tops + (int64_t)beam * p.segments + s + 32 * j) : -INFINITY;
+  };
+  const auto take_job = [&](int job) {
+#pragma unroll
+    for (int j = 0; j < kU; ++j) top[j] = next[j];
+    k = job / per_beam;
+    s0 = (job - k * per_beam) * 32 * kU + lane;
+    load_job(job + kWarps);
+    if (ended[k]) {  // one segment, whose logit is 0
+#pragma unroll
+      for (int j = 0; j < kU; ++j) top[j] = s0 + 32 * j == 0 ? 0.f : -INFINITY;
     }
   };
-  load_tops(0);
-  for (int k = warp; k < p.beams; k += kWarps) {  // a warp a beam
-    const float score = p.scores[r0 + k];
-    if (p.ended && p.ended[r0 + k]) {
-      if (lane == 0) base[k] = score;
-      continue;
+  load_job(warp);
+  {
+    float2 q = make_float2(-INFINITY, 0.f);
+    float score = 0.f;
+    bool over = false;
+    const auto load_beam = [&](int beam) {
+      if (beam >= p.beams) return;
+      score = p.scores[r0 + beam];
+      over = p.ended && p.ended[r0 + beam];
+      q = lane < p.slices ? __ldcg(p.part + (int64_t)(r0 + beam) * p.slices + lane) : make_float2(-INFINITY, 0.f);
+    };
+    load_beam(warp);
+    for (int beam = warp; beam < p.beams; beam += kWarps) {  // a warp a beam
+      const float plus = score;
+      const bool done = over;
+      float m = q.x, s = q.y;  // a lane's blocks, in turn
+      load_beam(beam + kWarps);
+      for (int i = lane + 32; i < p.slices && !done; i += 32) {
+        const float2 more = __ldcg(p.part + (int64_t)(r0 + beam) * p.slices + i);
+        const float now = fmaxf(m, more.x), ref = now == -INFINITY ? 0.f : now;
+        s = s * exp_of(m - ref) + more.y * exp_of(more.x - ref);
+        m = now;
+      }
+      const float most = warp_max_f(m);
+      s = warp_sum_f(s * exp_of(m - (most == -INFINITY ? 0.f : most)));
+      if (lane == 0) base[beam] = done ? plus : plus - (most + logf(s)), ended[beam] = done;
     }
-    const float2 *part = p.part + (int64_t)(r0 + k) * p.slices;
-    float m = -INFINITY, s = 0.f;  // a lane's blocks, in turn
-    for (int i = lane; i < p.slices; i += 32) {
-      const float2 q = __ldcg(part + i);
-      const float now = fmaxf(m, q.x), ref = now == -INFINITY ? 0.f : now;
-      s = s * exp_of(m - ref) + q.y * exp_of(q.x - ref);
-      m = now;
-    }
-    const float most = warp_max_f(m);
-    s = warp_sum_f(s * exp_of(m - (most == -INFINITY ? 0.f : most)));
-    if (lane == 0) base[k] = score - (most + logf(s));
   }
   if (t == 0) *list.count = 0;
   __syncthreads();
 
-  // Segment i % segments of beam i / segments; an ended beam is one segment, whose logit is 0.
-  const float per = 1.f / (float)p.segments;
-  const auto segment = [&](int i, float l) -> Entry {
-    if (i >= all) return {0, 0};
-    int k = (int)(((float)i + 0.5f) * per);  // (one off at most)
-    k -= k * p.segments > i;
-    k += (k + 1) * p.segments <= i;
-    const int s = i - k * p.segments;
-    if (p.ended && p.ended[r0 + k]) return s == 0 ? make_entry(base[k], k, 0.f, 0) : Entry{0, 0};
-    return make_entry(base[k], k, l, s);
-  };
-  Entry best = {0, 0}, mine[kU];
-  for (int at = 0; at < all; at += kU * kThreads) {
-    if (at > 0) load_tops(at);
+  // The n best segments.  A thread's best: its values in turn, which come by
+  // beam and number, so that a later one has to be larger (or, of one beam, to
+  // be a larger logit of the same rounded value).
+  float best_v = -INFINITY, best_l = -INFINITY;
+  int best_k = 0, best_s = 0;
+  for (int job = warp; job < jobs; job += kWarps) {
+    take_job(job);
+    const float plus = base[k];
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
-      mine[j] = segment(at + t + j * kThreads, top[j]);
-      if (above(mine[j], best)) best = mine[j];
+      const float v = plus + top[j];
+      if (v < INFINITY && (v > best_v || (v == best_v && k == best_k && top[j] > best_l)))
+        best_v = v, best_l = top[j], best_k = k, best_s = s0 + 32 * j;
     }
   }
-  Entry least = list.nth_of_groups(best);
+  Entry least = list.nth_of_groups(entry_of(best_v, best_k, best_l, best_s));
   while (true) {
-    for (int at = 0; at < all; at += kU * kThreads) {
-      if (all > kU * kThreads) {
-        load_tops(at);
-#pragma unroll
-        for (int j = 0; j < kU; ++j) mine[j] = segment(at + t + j * kThreads, top[j]);
-      }
+    const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
+    load_job(warp);
+    for (int job = warp; job < jobs; job += kWarps) {
+      take_job(job);
+      const float plus = base[k];
 #pragma unroll
       for (int j = 0; j < kU; ++j)
-        if (mine[j].v && !above(least, mine[j])) list.push(mine[j]);
+        if (plus + top[j] >= bar) {
+          const Entry e = make_entry(plus, k, top[j], s0 + 32 * j);
+          if (e.v && !above(least, e)) list.push(e);
+        }
     }
     __syncthreads();
     const bool over = *list.count > kList;
@@ -474,19 +495,19 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   // (As a candidate's, the threshold's token is the last of its segment.)
   least.k = (least.k & ~0xFFFFFFFFull) | (uint32_t)~((key_token(least.k) + 1) * kSegment - 1);
   // This lane's logits of the c-th segment, of beam k and from token v (an ended beam: a logit of 0 in place 0).
-  const auto load_segment = [&](int c, float(&x)[kE], int &k, int &v) {
+  const auto load_segment = [&](int c, float(&x)[kE], int &beam, int &v) {
 #pragma unroll
     for (int i = 0; i < kE; ++i) x[i] = -INFINITY;
-    k = v = 0;
+    beam = v = 0;
     if (c >= chosen) return;
     const Entry seg = best_segments[c];
-    k = (int)~(uint32_t)seg.v;
-    if (p.ended && p.ended[r0 + k]) {
+    beam = (int)~(uint32_t)seg.v;
+    if (ended[beam]) {
       if (lane == 0) x[0] = 0.f;
     } else {
       v = (int)key_token(seg.k) * kSegment;
       Raw<T> raw;
-      raw.load(static_cast<const T *>(p.logits) + (int64_t)(r0 + k) * p.ld, v, p.vocab, p.vec);
+      raw.load(static_cast<const T *>(p.logits) + (int64_t)(r0 + beam) * p.ld, v, p.vocab, p.vec);
       raw.values(x);
     }
   };
@@ -494,7 +515,7 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
   for (int c = warp; c < chosen; c += kWarps) {
     float x[kE];
-    int k, v;
+    int v;
     load_segment(c, x, k, v);
     const float plus = base[k];
 #pragma unroll
@@ -512,7 +533,7 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
     if (t == 0) *list.count = 0;
     for (int c = 0; c < chosen; c += kWarps) {
       float x[kE];
-      int k, v;
+      int v;
       load_segment(c + warp, x, k, v);
       const float plus = base[k];
       Entry top_entry = {0, 0};
@@ -541,9 +562,9 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
     const bool there = i < len;
     const Entry e = there ? list.item[i] : Entry{0, 0};
     p.out_scores[o] = there ? unordered((uint32_t)(e.v >> 32)) : -INFINITY;
-    const int k = there ? (int)~(uint32_t)e.v : -1;
+    k = there ? (int)~(uint32_t)e.v : -1;
     p.out_parents[o] = k;
-    p.out_tokens[o] = !there ? -1 : p.ended && p.ended[r0 + k] ? p.end_token : (int32_t)key_token(e.k);
+    p.out_tokens[o] = !there ? -1 : ended[k] ? p.end_token : (int32_t)key_token(e.k);
   }
 }
 
@@ -554,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
   extern __shared__ uint4 smem16[];
   __shared__ Entry groups[256], mark, best_segments[ARCHEAD_BEAM_MAX_OUT];
   __shared__ float red[ARCHEAD_BEAM_MAX_BEAMS];
+  __shared__ bool ended[ARCHEAD_BEAM_MAX_BEAMS];
   __shared__ int count, before;
   const int r = blockIdx.x / p.slices, sl = blockIdx.x - r * p.slices, b = r / p.beams;
   if (!(p.ended && p.ended[r])) reduce_slice<T>(p, r, sl, smem16, red);
@@ -565,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
   __threadfence();
   if (threadIdx.x == 0) p.counters[b] = 0;
   List list = {reinterpret_cast<Entry *>(smem16), groups, &mark, &count, p.n};
-  merge<T>(p, b, list, best_segments, red);
+  merge<T>(p, b, list, best_segments, red, ended);
 }
 
 }  // namespace

@@ -35,7 +35,6 @@ struct archead_int8_weight {
   uint8_t *codes = nullptr;
   float *scales = nullptr;
   int *err = nullptr;
-  int *counters = nullptr;  // of the K slices (zero between calls)
   void *ws = nullptr;
   size_t ws_bytes = 0;
   int64_t reserved_tokens = 0;  // every AUTO call of up to so many fits
@@ -80,13 +79,12 @@ bool int8_decode_fits(int64_t M, int K_pad);  // all M tokens in one launch
 
 // Tensor-memory kernel: how a product of M tokens is cut.
 struct I8GemmPlan {
-  int NT = 0, nt = 0, ks = 1;
+  int NT = 0, nt = 0, ks_log2 = 0;
   int64_t num_mt = 0, units = 0;
-  size_t partial_bytes = 0;
 };
 I8GemmPlan int8_gemm_plan(const archead_int8_weight *w, int64_t M);
-// x: widened token codes [M][K_pad]; partial: scratch of the plan's size.
+// x: widened token codes [M][K_pad].
 cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, const uint16_t *x,
-                             const float *x_scales, int64_t M, I8Out out, float *partial, cudaStream_t s);
+                             const float *x_scales, int64_t M, I8Out out, cudaStream_t s);
 
 }  // namespace archead

@@ -18,7 +18,7 @@ constexpr int kReserveTokens = 64;  // a new weight's workspace
 struct Plan {
   bool gemm = false, direct = false;
   I8GemmPlan g;
-  size_t x_off = 0, scale_off = 0, partial_off = 0, total = 0;
+  size_t x_off = 0, scale_off = 0, total = 0;
 };
 
 size_t take(size_t &off, size_t bytes) {
@@ -47,20 +47,17 @@ Plan plan(const archead_int8_weight *w, int64_t M, Given given, archead_path pat
   p.direct = !p.gemm && (given == kActivations ? int8_decode_quantizes(M, w->K, w->K_pad) : int8_decode_fits(1, w->K_pad));
   if (!p.direct) p.x_off = take(p.total, (size_t)M * w->K_pad * (p.gemm ? 2 : 1));
   if (!p.direct && given == kActivations) p.scale_off = take(p.total, (size_t)M * sizeof(float));
-  if (p.gemm) {
-    p.g = int8_gemm_plan(w, M);
-    p.partial_off = take(p.total, p.g.partial_bytes);
-  }
+  if (p.gemm) p.g = int8_gemm_plan(w, M);
   return p;
 }
 
-// The most that AUTO needs for up to M tokens.  K slices have the most partial
-// sums at the largest count of a tokens' tile.
+// The most that AUTO needs for up to M tokens: what it needs for M, or for the
+// most tokens that the warp-level kernel does not take as they are.
 size_t room_for(const archead_int8_weight *w, int64_t M) {
-  size_t most = 0;
-  for (int64_t m : {(int64_t)16, (int64_t)32, (int64_t)48, (int64_t)64, (int64_t)128, (int64_t)256, (int64_t)512, (int64_t)1024})
+  size_t most = plan(w, M, kActivations, ARCHEAD_PATH_AUTO).total;
+  for (int64_t m : {8, 16, 32})
     if (m < M) most = std::max(most, plan(w, m, kActivations, ARCHEAD_PATH_AUTO).total);
-  return std::max(most, plan(w, M, kActivations, ARCHEAD_PATH_AUTO).total);
+  return most;
 }
 
 // Growing synchronises the device: a call made earlier on another stream may
@@ -101,19 +98,16 @@ T *at(const archead_int8_weight *w, size_t off) {
   return reinterpret_cast<T *>(static_cast<char *>(w->ws) + off);
 }
 
-// One for each epilogue warp of the (tile, tokens) that K slices may share.
-size_t counter_bytes(const archead_int8_weight *w) { return (size_t)w->sm_count * 8 * sizeof(int); }
-
 // The product of token codes that have been laid out in the workspace.
 archead_status run_product(archead_int8_weight *w, const Plan &p, const float *x_scales, int64_t M, I8Out out,
                            cudaStream_t s) {
   if (p.gemm)
-    return status_of(launch_int8_gemm(w, p.g, at<uint16_t>(w, p.x_off), x_scales, M, out, at<float>(w, p.partial_off), s));
+    return status_of(launch_int8_gemm(w, p.g, at<uint16_t>(w, p.x_off), x_scales, M, out, s));
   return status_of(launch_int8_decode(w, at<int8_t>(w, p.x_off), 0, w->K_pad, x_scales, M, out, s));
 }
 
 void free_weight(archead_int8_weight *w) {
-  for (void *b : {(void *)w->codes, (void *)w->scales, (void *)w->err, (void *)w->counters, w->ws})
+  for (void *b : {(void *)w->codes, (void *)w->scales, (void *)w->err, w->ws})
     if (b) cudaFree(b);
   delete w;
 }
@@ -157,9 +151,6 @@ archead_status archead_int8_weight_create(const int8_t *codes, const float *scal
     if ((e = cudaMalloc(&w->err, 16)) != cudaSuccess) return e;
     w->owned_bytes = (int64_t)(code_bytes + scale_bytes + 16);
     if ((e = grow_workspace(w, room_for(w, kReserveTokens))) != cudaSuccess) return e;
-    if ((e = cudaMalloc(&w->counters, counter_bytes(w))) != cudaSuccess) return e;
-    w->owned_bytes += (int64_t)counter_bytes(w);
-    if ((e = cudaMemsetAsync(w->counters, 0, counter_bytes(w), s)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(w->err, 0, 16, s)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(w->scales, 0, scale_bytes, s)) != cudaSuccess) return e;
     if ((e = cudaMemcpyAsync(w->scales, scales, (size_t)N * sizeof(float), cudaMemcpyDefault, s)) != cudaSuccess)
@@ -260,10 +251,7 @@ archead_status archead_int8_sync_status(archead_int8_weight *w, void *stream) {
     set_last_error_message("a kernel found its shared-memory window misaligned for its TMA layout and skipped its work");
     return ARCHEAD_ERR_UNSUPPORTED;
   }
-  if (!(word & kErrWaitTimeout)) return ARCHEAD_OK;
-  // A call that gave up may have left its counters behind.
-  AH_TRY(cudaMemsetAsync(w->counters, 0, counter_bytes(w), s));
-  return ARCHEAD_ERR_DEVICE_TIMEOUT;
+  return word & kErrWaitTimeout ? ARCHEAD_ERR_DEVICE_TIMEOUT : ARCHEAD_OK;
 }
 
 archead_status archead_int8_set_wait_budget(archead_int8_weight *w, int64_t cycles) {

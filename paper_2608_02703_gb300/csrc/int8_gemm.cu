@@ -26,9 +26,10 @@
 
 namespace archead {
 
-// Instance for units of up to NT tokens.  TMEM: kAcc accumulators of NT
-// columns, then kA stages of the A operand (64 columns: 128 of K).
-template <int NT>
+// Instance for units of up to NT tokens; kSplit: the blocks of a cluster share
+// the K of one unit and join their sums.  TMEM: kAcc accumulators of NT columns,
+// then kA stages of the A operand (64 columns: 128 of K).
+template <int NT, bool kSplit>
 struct I8Geom {
   static constexpr int kAcc = 256 / NT;
   static constexpr int kConv = NT == 256 ? 2 : 4;  // converter warpgroups
@@ -38,11 +39,13 @@ struct I8Geom {
   static constexpr int kThreads = 128 * (1 + kConv + kEpi);
   static constexpr int kBoxBytes = NT * 64 * 2;
   static constexpr int kXBytes = 2 * kBoxBytes;
-  static constexpr int kXS = NT == 64 ? 6 : NT == 128 ? 4 : 2;
+  static constexpr int kXS = NT == 64 ? (kSplit ? 4 : 6) : NT == 128 ? (kSplit ? 3 : 4) : 2;
   static constexpr int kCodeSlot = kI8PadN * kI8PadK;  // 16 KB
-  static constexpr int kCS = NT == 64 ? 7 : 5;
+  static constexpr int kCS = NT == 64 ? 7 : NT == 128 && kSplit ? 4 : 5;
   static constexpr int kCodeOff = kXS * kXBytes;
-  static constexpr int kBarOff = kCodeOff + kCS * kCodeSlot;
+  static constexpr int kJoinOff = kCodeOff + kCS * kCodeSlot;  // sums of this block's tokens, from every block of the cluster
+  static constexpr int kJoinBytes = kSplit ? NT * kI8PadN * 4 : 0;
+  static constexpr int kBarOff = kJoinOff + kJoinBytes;
   static constexpr int kBars = 2 * kXS + 2 * kCS + 2 * kA + 2 * kAcc + 1;
   static constexpr int kSmem = kBarOff + kBars * 8 + 16;
   static constexpr int kRegs0 = NT == 256 ? 48 : 56;
@@ -61,10 +64,8 @@ struct I8GemmParams {
   I8Out out;
   int64_t N;
   int M, nt, num_mt, units;
-  int KC;    // stages of K
-  int ks;    // slices of K (units of their own, joined through `partial`)
-  float *partial;
-  int *counters;  // one a warp of each (tile, tokens), zero between calls
+  int KC;        // stages of K
+  int ks_log2;   // log2 of the blocks that share a unit's K
   int *err;
   int64_t wait_budget;
 };
@@ -100,9 +101,13 @@ __device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_
   }
 }
 
-template <int NT>
-__global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(const __grid_constant__ I8GemmParams p) {
-  using G = I8Geom<NT>;
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory"); }
+
+template <int NT, bool kSplit>
+__global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
+    int8_gemm_kernel(const __grid_constant__ I8GemmParams p) {
+  using G = I8Geom<NT, kSplit>;
   constexpr int kXS = G::kXS, kCS = G::kCS, kA = G::kA, kAcc = G::kAcc;
   extern __shared__ uint8_t smem[];  // 1024-byte aligned (the swizzle's period)
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + G::kBarOff);
@@ -134,9 +139,12 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
   const uint32_t a_base = tmem_base + kAcc * NT;
   bool mma_leader = false;
 
-  // Unit u: K slice u % ks, tokens (u / ks) % num_mt, tile u / ks / num_mt.
-  const auto k_begin = [&](int u) { return (int)((int64_t)p.KC * (u % p.ks) / p.ks); };
-  const auto k_end = [&](int u) { return (int)((int64_t)p.KC * (u % p.ks + 1) / p.ks); };
+  // Unit u: tokens u % num_mt of tile u / num_mt.  With kSplit a cluster has one
+  // unit and this block one slice of its K.
+  const int ks = kSplit ? 1 << p.ks_log2 : 1, slice = kSplit ? (int)blockIdx.x & (ks - 1) : 0;
+  const int u0 = kSplit ? (int)blockIdx.x >> p.ks_log2 : (int)blockIdx.x, step = kSplit ? p.units : (int)gridDim.x;
+  const int begin = kSplit ? p.KC * slice / ks : 0, end = kSplit ? p.KC * (slice + 1) / ks : p.KC;
+  bool at_barrier = false;  // this thread has met the cluster
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegs0) : "memory");
@@ -146,9 +154,9 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
       RingPos<kXS> r;
       int issued = 0;
       asm volatile("griddepcontrol.wait;\n" ::: "memory");  // the widened codes come from the grid before
-      for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-        const int m0 = u / p.ks % p.num_mt * p.nt, end = k_end(u);
-        for (int e = k_begin(u); e < end; ++e) {
+      for (int u = u0; u < p.units; u += step) {
+        const int m0 = u % p.num_mt * p.nt;
+        for (int e = begin; e < end; ++e) {
           if (!mbar_wait_warp(&x_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
             drain_copies(x_full, kXS, issued, p.wait_budget, p.err);
             goto done;
@@ -169,10 +177,9 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
       const bool leader = elect_one();
       RingPos<kCS> r;
       int issued = 0;
-      for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-        const uint8_t *src = p.codes + (int64_t)(u / p.ks / p.num_mt) * p.KC * G::kCodeSlot;
-        const int end = k_end(u);
-        for (int e = k_begin(u); e < end; ++e) {
+      for (int u = u0; u < p.units; u += step) {
+        const uint8_t *src = p.codes + (int64_t)(u / p.num_mt) * p.KC * G::kCodeSlot;
+        for (int e = begin; e < end; ++e) {
           if (!mbar_wait_warp(&c_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
             drain_copies(c_full, kCS, issued, p.wait_budget, p.err);
             goto done;
@@ -197,8 +204,7 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
       RingPos<kXS> xr;
       RingPos<kA> ar;
       RingPos<kAcc> accr;
-      for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-        const int begin = k_begin(u), end = k_end(u);
+      for (int u = u0; u < p.units; u += step) {
         if (!mbar_wait_warp(&acc_empty[accr.s], accr.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
         const uint32_t d = tmem_base + accr.s * NT;
         for (int e = begin; e < end; ++e) {
@@ -231,8 +237,8 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
     cr.next(cg);
     ar.next(cg);
     int n = cg;  // this warpgroup's next stage, of the stages of unit u
-    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-      const int len = k_end(u) - k_begin(u);
+    for (int u = u0; u < p.units; u += step) {
+      const int len = end - begin;
       for (; n < len; n += G::kConv) {
         // The A stage first: that it is free says that all stages up to n - kA
         // are converted, so with kCS >= kA slots the code slot's barrier is at
@@ -281,10 +287,9 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
     const uint32_t lane_addr = tmem_base + ((uint32_t)(lg * 32) << 16) + col0;
     RingPos<kAcc> accr;
     asm volatile("griddepcontrol.wait;\n" ::: "memory");  // (the tokens' scales)
-    for (int u = blockIdx.x; u < p.units; u += gridDim.x) {
-      const int t = u / p.ks, slice = u % p.ks;
-      const int64_t n = (int64_t)(t / p.num_mt) * kI8PadN + lg * 32 + lane;
-      const int mu = t % p.num_mt * p.nt;
+    for (int u = u0; u < p.units; u += step) {
+      const int64_t n = (int64_t)(u / p.num_mt) * kI8PadN + lg * 32 + lane;
+      const int mu = u % p.num_mt * p.nt;
       const int m0 = mu + col0, cols = min(kCols, min(p.M, mu + p.nt) - m0);  // (may be negative: none)
       const float sw = p.scales[n];
       float xs[kCols / 32];
@@ -305,28 +310,34 @@ __global__ void __launch_bounds__(I8Geom<NT>::kThreads, 1) int8_gemm_kernel(cons
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[accr.s]);
       accr.next();
-      if (p.ks > 1) {
-        // The slice's sums; the warp that comes last of a (tile, tokens) adds
-        // them up in the order of the slices.
-        float *part = p.partial + ((int64_t)t * p.ks * NT + col0) * kI8PadN + lg * 32 + lane;
+      if constexpr (kSplit) {
+        // Block q of the cluster takes the tokens from q NT / ks on: the sums go
+        // into its shared memory, by slice, and after the cluster's barrier it
+        // adds them up in the order of the slices.
+        const int per_log2 = (NT == 64 ? 6 : 7) - p.ks_log2, per = 1 << per_log2;
+        const uint32_t join = smem_u32(smem) + G::kJoinOff;
+        const uint32_t mine = (slice * per * kI8PadN + lg * 32 + lane) * 4;
 #pragma unroll
-        for (int i = 0; i < kCols; ++i)
-          if (i < cols) __stcg(part + ((int64_t)slice * NT + i) * kI8PadN, acc[i]);
-        __threadfence();
-        __syncwarp();
-        int before = 0;
-        int *counter = p.counters + (int64_t)t * 4 * G::kEpi + 4 * pw + lg;
-        if (lane == 0) before = atomicAdd(counter, 1);
-        before = __shfl_sync(0xffffffffu, before, 0);
-        if (before != p.ks - 1) continue;
-        __threadfence();
-        if (lane == 0) *counter = 0;
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
-        for (int s = 0; s < p.ks; ++s)
-#pragma unroll
-          for (int i = 0; i < kCols; ++i)
-            if (i < cols) acc[i] += __ldcg(part + ((int64_t)s * NT + i) * kI8PadN);
+        for (int i = 0; i < kCols; ++i) {
+          const int c = col0 + i;
+          uint32_t to;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(to) : "r"(join), "r"(c >> per_log2));
+          if (i < cols)
+            asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(to + mine + (c & (per - 1)) * (kI8PadN * 4)), "f"(acc[i])
+                         : "memory");
+        }
+        cluster_arrive();
+        cluster_wait();
+        at_barrier = true;
+        const int lim = min(per, min(p.M, mu + p.nt) - mu - slice * per);  // tokens of this block
+        const float *sums = reinterpret_cast<const float *>(smem + G::kJoinOff) + lg * 32 + lane;
+        const int64_t mb = mu + slice * per;
+        for (int i = pw; i < lim && n < p.N; i += G::kEpi) {
+          float v = 0.f;
+          for (int s = 0; s < ks; ++s) v += sums[(s * per + i) * kI8PadN];
+          store_i8_out(p.out, mb + i, n, v * p.x_scales[mb + i] * sw);
+        }
+        break;
       }
       const bool there = n < p.N;
       if (p.out.dtype == ARCHEAD_DTYPE_FP32)
@@ -342,6 +353,11 @@ done:
     tc_commit(drain);
     mbar_wait(drain, 0, p.wait_budget, nullptr, p.err);
   }
+  if (kSplit && !at_barrier) {  // every thread meets its cluster once, whatever became of its work
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -352,44 +368,65 @@ done:
 
 namespace {
 
-template <int NT>
+template <int NT, bool kSplit>
 cudaError_t launch_gemm_t(const I8GemmParams &p, int grid, cudaStream_t s) {
-  auto kern = int8_gemm_kernel<NT>;
-  cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), I8Geom<NT>::kSmem);
+  auto kern = int8_gemm_kernel<NT, kSplit>;
+  using G = I8Geom<NT, kSplit>;
+  cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), G::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(I8Geom<NT>::kThreads);
-  cfg.dynamicSmemBytes = I8Geom<NT>::kSmem;
+  cfg.blockDim = dim3(G::kThreads);
+  cfg.dynamicSmemBytes = G::kSmem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1 << p.ks_log2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = kSplit ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 }  // namespace
 
+// How a product is cut: the least estimated time over the instances (64, 128 or
+// 256 tokens a unit, spread evenly) and, for units too few for the
+// multiprocessors, clusters of 2, 4 or 8 blocks along K.  In cycles: a stage's
+// eight MMAs of nt tokens, or what its other roles take; a unit's epilogue; a
+// cluster's join.
 I8GemmPlan int8_gemm_plan(const archead_int8_weight *w, int64_t M) {
-  I8GemmPlan f;
-  f.NT = M <= 64 ? 64 : M <= 128 ? 128 : 256;
+  I8GemmPlan best;
+  double least = 1e300;
   const int64_t tiles = w->N_pad / kI8PadN;
-  f.num_mt = (M + f.NT - 1) / f.NT;
-  f.nt = (int)(((M + f.num_mt - 1) / f.num_mt + 15) / 16 * 16);
-  const int64_t pairs = tiles * f.num_mt;
   const int KC = w->K_pad / kI8PadK;
-  // Too few (tile, tokens) for the multiprocessors: K in slices of at least four stages.
-  f.ks = 1;
-  if (pairs * 2 <= w->sm_count) f.ks = (int)std::max<int64_t>(1, std::min<int64_t>({w->sm_count / pairs, KC / 4, 8}));
-  f.units = pairs * f.ks;
-  if (f.ks > 1) f.partial_bytes = (size_t)f.units * f.NT * kI8PadN * sizeof(float);
-  return f;
+  for (int NT = 64; NT <= 256; NT *= 2) {
+    const int64_t num_mt = (M + NT - 1) / NT;
+    const int nt = (int)(((M + num_mt - 1) / num_mt + 15) / 16 * 16);
+    const int64_t units = tiles * num_mt;
+    for (int ks_log2 = 0; ks_log2 <= (NT == 256 ? 0 : 3) && 2 << ks_log2 <= 2 * KC; ++ks_log2) {
+      const int64_t blocks = units << ks_log2;
+      if (ks_log2 > 0 && blocks > w->sm_count) break;  // (a cluster has one unit)
+      const double rounds = (double)((blocks + w->sm_count - 1) / w->sm_count);
+      const double stage = std::max(4.0 * nt + 40, 400.0), stages = (KC + (1 << ks_log2) - 1) >> ks_log2;
+      const double cost = rounds * stages * stage + 10.0 * nt + (ks_log2 > 0 ? 2500 : 0);
+      if (cost < least) {
+        least = cost;
+        best.NT = NT;
+        best.nt = nt;
+        best.ks_log2 = ks_log2;
+        best.num_mt = num_mt;
+        best.units = units;
+      }
+    }
+  }
+  return best;
 }
 
 cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, const uint16_t *x,
-                             const float *x_scales, int64_t M, I8Out out, float *partial, cudaStream_t s) {
+                             const float *x_scales, int64_t M, I8Out out, cudaStream_t s) {
   I8GemmParams p{};
   if (!make_tma_map_bf16(&p.tmap_x, x, M, w->K_pad, f.nt)) return cudaErrorInvalidValue;
   if (f.units > 0x7fffffff - w->sm_count) return cudaErrorInvalidValue;
@@ -403,13 +440,17 @@ cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, 
   p.num_mt = (int)f.num_mt;
   p.units = (int)f.units;
   p.KC = w->K_pad / kI8PadK;
-  p.ks = f.ks;
-  p.partial = partial;
-  p.counters = w->counters;
+  p.ks_log2 = f.ks_log2;
   p.err = w->err;
   p.wait_budget = w->wait_budget;
+  if (f.ks_log2 > 0) {
+    const int grid = (int)f.units << f.ks_log2;
+    return f.NT == 64 ? launch_gemm_t<64, true>(p, grid, s) : launch_gemm_t<128, true>(p, grid, s);
+  }
   const int grid = (int)std::min<int64_t>(f.units, w->sm_count);
-  return f.NT == 64 ? launch_gemm_t<64>(p, grid, s) : f.NT == 128 ? launch_gemm_t<128>(p, grid, s) : launch_gemm_t<256>(p, grid, s);
+  return f.NT == 64    ? launch_gemm_t<64, false>(p, grid, s)
+         : f.NT == 128 ? launch_gemm_t<128, false>(p, grid, s)
+                       : launch_gemm_t<256, false>(p, grid, s);
 }
 
 }  // namespace archead
