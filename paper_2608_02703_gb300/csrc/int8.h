@@ -35,6 +35,7 @@ struct archead_int8_weight {
   uint8_t *codes = nullptr;
   float *scales = nullptr;
   int *err = nullptr;
+  int clusters[2][4] = {};  // of 2^i blocks of the split tensor-memory kernels (64, 128 tokens) that run at once
   void *ws = nullptr;
   size_t ws_bytes = 0;
   int64_t reserved_tokens = 0;  // every AUTO call of up to so many fits
@@ -82,6 +83,7 @@ struct I8GemmPlan {
   int NT = 0, nt = 0, ks_log2 = 0;
   int64_t num_mt = 0, units = 0;
 };
+cudaError_t int8_gemm_room(archead_int8_weight *w);  // fills w->clusters
 I8GemmPlan int8_gemm_plan(const archead_int8_weight *w, int64_t M);
 // x: widened token codes [M][K_pad].
 cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, const uint16_t *x,

@@ -300,18 +300,19 @@ cudaError_t launch_int8_decode(const archead_int8_weight *w, const void *x, int 
   p.ldx = ldx;
   p.err = w->err;
   p.wait_budget = w->wait_budget;
-  // K stages a slot: the fewest bytes for the busiest block, where a round's end
-  // costs about as much as half a slot.
+  // K stages a slot: the fewest slots for the busiest block, where a round's end
+  // costs about as much as one and a half.
   const int64_t all = (w->N + kI8Strip - 1) / kI8Strip;
   double least = 1e30;
   for (int kw = 1; kw <= 8; kw *= 2) {
     const int64_t per_round = (int64_t)w->sm_count * (8 / kw), rounds = (all + per_round - 1) / per_round;
-    const double cost = rounds * ((double)p.KC / kw + 0.5);
+    const int steps = (p.KC + kw - 1) / kw;
+    const double cost = rounds * (steps + 1.5);
     if (cost < least) {
       least = cost;
       p.kw = kw;
       p.rounds = (int)rounds;
-      p.steps = (p.KC + kw - 1) / kw;
+      p.steps = steps;
     }
   }
   const int strips = 8 / p.kw;

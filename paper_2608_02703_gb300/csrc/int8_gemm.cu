@@ -29,17 +29,23 @@ namespace archead {
 // Instance for units of up to NT tokens; kSplit: the blocks of a cluster share
 // the K of one unit and join their sums.  TMEM: kAcc accumulators of NT columns,
 // then kA stages of the A operand (64 columns: 128 of K).
+//
+// Up to 128 tokens a unit, the x ring and the A ring are one: a stage's barrier
+// completes with its x and its A operand, and the MMAs' commit frees both.  A
+// satisfied barrier probe takes some 90 cycles, and with one for each the issuing
+// thread needed longer for a stage than its MMAs.
 template <int NT, bool kSplit>
 struct I8Geom {
-  static constexpr int kAcc = 256 / NT;
-  static constexpr int kConv = NT == 256 ? 2 : 4;  // converter warpgroups
-  static constexpr int kA = 4;                     // A stages
+  static constexpr bool kOne = NT <= 128;
+  static constexpr int kConv = NT == 256 ? 2 : NT == 128 && kSplit ? 3 : 4;  // converter warpgroups
+  static constexpr int kXS = NT == 64 ? (kSplit ? 4 : 6) : NT == 128 ? (kSplit ? 3 : 4) : 2;
+  static constexpr int kA = kOne ? kXS : 4;        // A stages
+  static constexpr int kAcc = NT == 64 ? 2 : 256 / NT;
   static constexpr int kEpi = NT == 64 ? 1 : 2;    // epilogue warpgroups
   static constexpr int kCols = NT / kEpi;          // accumulator columns a thread takes
   static constexpr int kThreads = 128 * (1 + kConv + kEpi);
   static constexpr int kBoxBytes = NT * 64 * 2;
   static constexpr int kXBytes = 2 * kBoxBytes;
-  static constexpr int kXS = NT == 64 ? (kSplit ? 4 : 6) : NT == 128 ? (kSplit ? 3 : 4) : 2;
   static constexpr int kCodeSlot = kI8PadN * kI8PadK;  // 16 KB
   static constexpr int kCS = NT == 64 ? 7 : NT == 128 && kSplit ? 4 : 5;
   static constexpr int kCodeOff = kXS * kXBytes;
@@ -49,12 +55,12 @@ struct I8Geom {
   static constexpr int kBars = 2 * kXS + 2 * kCS + 2 * kA + 2 * kAcc + 1;
   static constexpr int kSmem = kBarOff + kBars * 8 + 16;
   static constexpr int kRegs0 = NT == 256 ? 48 : 56;
-  static constexpr int kRegsC = NT == 64 ? 72 : 56;
-  static constexpr int kRegsP = NT == 64 ? 128 : NT == 128 ? 112 : 160;
+  static constexpr int kRegsC = NT == 64 || kConv == 3 ? 72 : 56;
+  static constexpr int kRegsP = NT == 64 ? 128 : NT == 128 ? (kSplit ? 104 : 112) : 160;
   static_assert(128 * (kRegs0 + kConv * kRegsC + kEpi * kRegsP) <= 65536 / kThreads / 8 * 8 * kThreads, "registers");
   static_assert(kAcc * NT + kA * 64 <= kPfTmemCols, "TMEM columns");
   static_assert(kSmem <= 227 * 1024, "shared memory");
-  static_assert(kCS >= kA, "code slots (see the converters)");
+  static_assert(kA >= kConv && kCS >= kA, "stages and slots (see the converters)");
 };
 
 struct I8GemmParams {
@@ -72,6 +78,16 @@ struct I8GemmParams {
 
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// One probe of a barrier's phase, without suspending.
+__device__ __forceinline__ bool mbar_test_a(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity)
+               : "memory");
+  return ok != 0;
 }
 
 // Four signed codes as two fp16 pairs, exact: the offset-binary byte u in the
@@ -92,13 +108,24 @@ __device__ __forceinline__ void widen_int8x4(uint32_t w, uint32_t &lo, uint32_t 
 // to the same place: 256 tokens of 4096 x 512 took 13 us, now TODO.)
 template <typename T, int kCols>
 __device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_t n, bool there, const float (&acc)[kCols],
-                                              int cols, const float (&xs)[kCols / 32], float sw) {
+                                              int cols, const float (&xs)[(kCols + 31) / 32], float sw) {
   T *y = static_cast<T *>(o.y) + m0 * o.ld + n;
 #pragma unroll
   for (int i = 0; i < kCols; ++i, y += o.ld) {
     const float s = __shfl_sync(0xffffffffu, xs[i / 32], i % 32);
     if (there && i < cols) *y = from_f32<T>(acc[i] * s * sw);
   }
+}
+
+template <int kCols>
+__device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_t n, bool there, const float (&acc)[kCols],
+                                              int cols, const float (&xs)[(kCols + 31) / 32], float sw) {
+  if (o.dtype == ARCHEAD_DTYPE_FP32)
+    store_channel<float>(o, m0, n, there, acc, cols, xs, sw);
+  else if (o.dtype == ARCHEAD_DTYPE_FP16)
+    store_channel<__half>(o, m0, n, there, acc, cols, xs, sw);
+  else
+    store_channel<__nv_bfloat16>(o, m0, n, there, acc, cols, xs, sw);
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory"); }
@@ -114,6 +141,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
   uint64_t *x_full = bars, *x_empty = x_full + kXS, *c_full = x_empty + kXS, *c_empty = c_full + kCS;
   uint64_t *a_full = c_empty + kCS, *a_empty = a_full + kA, *acc_full = a_empty + kA, *acc_empty = acc_full + kAcc;
   uint64_t *drain = acc_empty + kAcc;
+  if (G::kOne) x_full = a_full, x_empty = a_empty;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = lane_id();
@@ -123,9 +151,9 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     return;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kXS; ++i) mbar_init(&x_full[i], 1), mbar_init(&x_empty[i], 1);
+    for (int i = 0; i < kXS && !G::kOne; ++i) mbar_init(&x_full[i], 1), mbar_init(&x_empty[i], 1);
     for (int i = 0; i < kCS; ++i) mbar_init(&c_full[i], 1), mbar_init(&c_empty[i], 4);
-    for (int i = 0; i < kA; ++i) mbar_init(&a_full[i], 4), mbar_init(&a_empty[i], 1);
+    for (int i = 0; i < kA; ++i) mbar_init(&a_full[i], G::kOne ? 5 : 4), mbar_init(&a_empty[i], 1);
     for (int i = 0; i < kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4 * G::kEpi);
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -204,26 +232,36 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       RingPos<kXS> xr;
       RingPos<kA> ar;
       RingPos<kAcc> accr;
+      bool polled = false;  // the next stage's barrier was seen complete
       for (int u = u0; u < p.units; u += step) {
         if (!mbar_wait_warp(&acc_empty[accr.s], accr.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
         const uint32_t d = tmem_base + accr.s * NT;
         for (int e = begin; e < end; ++e) {
-          if (!mbar_wait_warp(&x_full[xr.s], xr.ph, p.wait_budget, abort_flag, p.err)) goto done;
-          if (!mbar_wait_warp(&a_full[ar.s], ar.ph, p.wait_budget, abort_flag, p.err)) goto done;
+          if (!G::kOne && !mbar_wait_warp(&x_full[xr.s], xr.ph, p.wait_budget, abort_flag, p.err)) goto done;
+          if (!__all_sync(0xffffffffu, polled) &&
+              !mbar_wait_warp(&a_full[ar.s], ar.ph, p.wait_budget, abort_flag, p.err))
+            goto done;
           tc_fence_after();
+          const uint32_t a = a_base + ar.s * 64;
+          const uint64_t b = xdesc + (uint32_t)((G::kOne ? ar.s : xr.s) * (G::kXBytes >> 4));
+          const RingPos<kA> now = ar;
+          ar.next();
           if (leader) {
-            const uint32_t a = a_base + ar.s * 64;
-            const uint64_t b = xdesc + (uint32_t)(xr.s * (G::kXBytes >> 4));
 #pragma unroll
-            for (int q = 0; q < 8; ++q)  // (+2 in the descriptor: 32 bytes)
-              tc_mma_ts(d, a + 8 * q, b + (q >> 2) * kBox + 2 * (q & 3), idesc, q > 0 || e > begin);
-            tc_commit(&x_empty[xr.s]);
-            tc_commit(&a_empty[ar.s]);
+            for (int q = 0; q < 4; ++q)  // (+2 in the descriptor: 32 bytes)
+              tc_mma_ts(d, a + 8 * q, b + 2 * q, idesc, q > 0 || e > begin);
+          }
+          __syncwarp();
+          polled = mbar_test_a(smem_u32(&a_full[ar.s]), ar.ph);  // (under way while the others are issued)
+          if (leader) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tc_mma_ts(d, a + 8 * (q + 4), b + kBox + 2 * q, idesc, 1);
+            if (!G::kOne) tc_commit(&x_empty[xr.s]);
+            tc_commit(&a_empty[now.s]);
             if (e + 1 == end) tc_commit(&acc_full[accr.s]);
           }
           __syncwarp();
           xr.next();
-          ar.next();
         }
         accr.next();
       }
@@ -235,14 +273,17 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     RingPos<kCS> cr;
     RingPos<kA> ar;
     cr.next(cg);
-    ar.next(cg);
+    ar.next(cg);  // (cg < kConv <= kA)
     int n = cg;  // this warpgroup's next stage, of the stages of unit u
     for (int u = u0; u < p.units; u += step) {
       const int len = end - begin;
       for (; n < len; n += G::kConv) {
-        // The A stage first: that it is free says that all stages up to n - kA
-        // are converted, so with kCS >= kA slots the code slot's barrier is at
-        // most one phase from this stage's (a parity shows no more).
+        // A parity shows only one phase from the next, so a barrier may be at most
+        // one behind what is waited for.  The A stage's: this warpgroup's last
+        // stage n - kConv waited for the MMAs of n - kConv - kA, which with kA >=
+        // kConv are behind those that used this stage before the last.  Then the
+        // code slot's: that the A stage is free says that all stages up to n -
+        // kA are converted, so kCS >= kA.
         if (!mbar_wait_warp(&a_empty[ar.s], ar.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
         if (!mbar_wait_warp(&c_full[cr.s], cr.ph, p.wait_budget, abort_flag, p.err)) goto done;
         tc_fence_after();
@@ -273,8 +314,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&c_empty[cr.s]), mbar_arrive(&a_full[ar.s]);
         cr.next(G::kConv);
-        ar.next(G::kConv % kA);
-        if (G::kConv == kA) ar.ph ^= 1;
+        ar.next(G::kConv);
       }
       n -= len;
     }
@@ -294,7 +334,8 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       const float sw = p.scales[n];
       float xs[kCols / 32];
 #pragma unroll
-      for (int c = 0; c < kCols / 32; ++c) xs[c] = 32 * c + lane < cols ? p.x_scales[m0 + 32 * c + lane] : 0.f;
+      for (int c = 0; c < kCols / 32; ++c)
+        xs[c] = 32 * c + lane < cols ? p.x_scales[m0 + 32 * c + lane] : 0.f;
       if (!mbar_wait_warp(&acc_full[accr.s], accr.ph, p.wait_budget, abort_flag, p.err)) goto done;
       tc_fence_after();
       float acc[kCols];
@@ -313,39 +354,46 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       if constexpr (kSplit) {
         // Block q of the cluster takes the tokens from q NT / ks on: the sums go
         // into its shared memory, by slice, and after the cluster's barrier it
-        // adds them up in the order of the slices.
-        const int per_log2 = (NT == 64 ? 6 : 7) - p.ks_log2, per = 1 << per_log2;
-        const uint32_t join = smem_u32(smem) + G::kJoinOff;
-        const uint32_t mine = (slice * per * kI8PadN + lg * 32 + lane) * 4;
+        // adds them up in the order of the slices.  (The number of slices is a
+        // constant in each copy of this: with shifts and branches for every
+        // token a join took 3 to 7 us.)
+        const auto join = [&](auto log2) {
+          constexpr int kS = 1 << decltype(log2)::value, kPer = NT / kS, kMine = kPer / G::kEpi;
+          const uint32_t place = smem_u32(smem) + G::kJoinOff + (slice * kPer * kI8PadN + lg * 32 + lane) * 4;
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) {
-          const int c = col0 + i;
-          uint32_t to;
-          asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(to) : "r"(join), "r"(c >> per_log2));
-          if (i < cols)
-            asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(to + mine + (c & (per - 1)) * (kI8PadN * 4)), "f"(acc[i])
-                         : "memory");
-        }
-        cluster_arrive();
-        cluster_wait();
-        at_barrier = true;
-        const int lim = min(per, min(p.M, mu + p.nt) - mu - slice * per);  // tokens of this block
-        const float *sums = reinterpret_cast<const float *>(smem + G::kJoinOff) + lg * 32 + lane;
-        const int64_t mb = mu + slice * per;
-        for (int i = pw; i < lim && n < p.N; i += G::kEpi) {
-          float v = 0.f;
-          for (int s = 0; s < ks; ++s) v += sums[(s * per + i) * kI8PadN];
-          store_i8_out(p.out, mb + i, n, v * p.x_scales[mb + i] * sw);
-        }
+          for (int q = 0; q < kCols / kPer; ++q) {
+            if (q * kPer >= cols) break;
+            uint32_t to;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(to) : "r"(place), "r"(pw * (kCols / kPer) + q));
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+              asm volatile("st.shared::cluster.f32 [%0], %1;\n" ::"r"(to + i * (kI8PadN * 4)), "f"(acc[q * kPer + i])
+                           : "memory");
+          }
+          const int64_t mb = mu + slice * kPer + pw * kMine;
+          const int lim = min(p.M, mu + p.nt) - (int)mb;  // tokens of this thread (none or less: none)
+          float xq[(kMine + 31) / 32], v[kMine];
+#pragma unroll
+          for (int c = 0; c < (kMine + 31) / 32; ++c)
+            xq[c] = 32 * c + lane < min(lim, kMine) ? p.x_scales[mb + 32 * c + lane] : 0.f;
+          cluster_arrive();
+          cluster_wait();
+          at_barrier = true;
+          const float *sums = reinterpret_cast<const float *>(smem + G::kJoinOff) + pw * kMine * kI8PadN + lg * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) v[i] = sums[i * kI8PadN];
+#pragma unroll
+          for (int s = 1; s < kS; ++s)
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) v[i] += sums[(s * kPer + i) * kI8PadN];
+          store_channel<kMine>(p.out, mb, n, n < p.N, v, lim, xq, sw);
+        };
+        if (p.ks_log2 == 1) join(Int<1>{});
+        else if (p.ks_log2 == 2) join(Int<2>{});
+        else join(Int<3>{});
         break;
       }
-      const bool there = n < p.N;
-      if (p.out.dtype == ARCHEAD_DTYPE_FP32)
-        store_channel<float>(p.out, m0, n, there, acc, cols, xs, sw);
-      else if (p.out.dtype == ARCHEAD_DTYPE_FP16)
-        store_channel<__half>(p.out, m0, n, there, acc, cols, xs, sw);
-      else
-        store_channel<__nv_bfloat16>(p.out, m0, n, there, acc, cols, xs, sw);
+      store_channel<kCols>(p.out, m0, n, n < p.N, acc, cols, xs, sw);
     }
   }
 done:
@@ -392,34 +440,66 @@ cudaError_t launch_gemm_t(const I8GemmParams &p, int grid, cudaStream_t s) {
 
 }  // namespace
 
-// How a product is cut: the least estimated time over the instances (64, 128 or
-// 256 tokens a unit, spread evenly) and, for units too few for the
-// multiprocessors, clusters of 2, 4 or 8 blocks along K.  In cycles: a stage's
-// eight MMAs of nt tokens, or what its other roles take; a unit's epilogue; a
-// cluster's join.
+template <int NT>
+static cudaError_t clusters_of(int (&room)[4]) {
+  using G = I8Geom<NT, true>;
+  auto kern = int8_gemm_kernel<NT, true>;
+  cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), G::kSmem);
+  for (int log2 = 1; log2 <= 3 && e == cudaSuccess; ++log2) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1 << log2);
+    cfg.blockDim = dim3(G::kThreads);
+    cfg.dynamicSmemBytes = G::kSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1 << log2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&room[log2], kern, &cfg);
+  }
+  return e;
+}
+
+cudaError_t int8_gemm_room(archead_int8_weight *w) {
+  cudaError_t e = clusters_of<64>(w->clusters[0]);
+  if (e == cudaSuccess) e = clusters_of<128>(w->clusters[1]);
+  return e;
+}
+
+// How a product is cut: the least estimated time over the instances (units of up
+// to 64, 128 or 256 tokens, spread evenly) and over clusters of 1, 2, 4 or 8
+// blocks along K.  The estimate, in ns, goes by measured times of 4 to 32 stages
+// (128 of K): a stage of up to 64 tokens takes some 267, of 128 358 where many
+// blocks run (317 where few do), of 256 683; the start and the last epilogue 3 a
+// token and more for the larger instances; a join 1300.
 I8GemmPlan int8_gemm_plan(const archead_int8_weight *w, int64_t M) {
   I8GemmPlan best;
   double least = 1e300;
   const int64_t tiles = w->N_pad / kI8PadN;
   const int KC = w->K_pad / kI8PadK;
   for (int NT = 64; NT <= 256; NT *= 2) {
-    const int64_t num_mt = (M + NT - 1) / NT;
-    const int nt = (int)(((M + num_mt - 1) / num_mt + 15) / 16 * 16);
-    const int64_t units = tiles * num_mt;
-    for (int ks_log2 = 0; ks_log2 <= (NT == 256 ? 0 : 3) && 2 << ks_log2 <= 2 * KC; ++ks_log2) {
-      const int64_t blocks = units << ks_log2;
-      if (ks_log2 > 0 && blocks > w->sm_count) break;  // (a cluster has one unit)
-      const double rounds = (double)((blocks + w->sm_count - 1) / w->sm_count);
-      const double stage = std::max(4.0 * nt + 40, 400.0), stages = (KC + (1 << ks_log2) - 1) >> ks_log2;
-      const double cost = rounds * stages * stage + 10.0 * nt + (ks_log2 > 0 ? 2500 : 0);
-      if (cost < least) {
-        least = cost;
-        best.NT = NT;
-        best.nt = nt;
-        best.ks_log2 = ks_log2;
-        best.num_mt = num_mt;
-        best.units = units;
+    const int64_t fewest = (M + NT - 1) / NT;
+    for (int64_t num_mt = fewest; num_mt < fewest + 3; ++num_mt) {
+      const int nt = (int)(((M + num_mt - 1) / num_mt + 15) / 16 * 16);
+      const int64_t units = tiles * num_mt;
+      const double stage = NT == 64 ? 250 + 0.3 * nt : NT == 128 ? std::max(300.0, 217 + 1.1 * nt) : std::max(420.0, 120 + 2.2 * nt);
+      const double start = 3 * nt + (NT == 64 ? 0 : NT == 128 ? 300 : 1000);
+      for (int log2 = 0; log2 <= (NT == 256 ? 0 : 3) && 1 << log2 <= KC; ++log2) {
+        const int64_t at_once = log2 == 0 ? w->sm_count : w->clusters[NT == 128][log2];
+        if (at_once < 1) continue;
+        const double rounds = (double)((units + at_once - 1) / at_once);
+        const double cost = rounds * ((KC + (1 << log2) - 1) >> log2) * stage + start + (log2 > 0 ? 1300 * rounds : 0);
+        if (cost < least) {
+          least = cost;
+          best.NT = NT;
+          best.nt = nt;
+          best.ks_log2 = log2;
+          best.num_mt = num_mt;
+          best.units = units;
+        }
       }
+      if (nt <= 16) break;
     }
   }
   return best;
@@ -429,7 +509,7 @@ cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, 
                              const float *x_scales, int64_t M, I8Out out, cudaStream_t s) {
   I8GemmParams p{};
   if (!make_tma_map_bf16(&p.tmap_x, x, M, w->K_pad, f.nt)) return cudaErrorInvalidValue;
-  if (f.units > 0x7fffffff - w->sm_count) return cudaErrorInvalidValue;
+  if (f.units << f.ks_log2 > 0x7fffffff - w->sm_count) return cudaErrorInvalidValue;
   p.codes = w->codes;
   p.scales = w->scales;
   p.x_scales = x_scales;
