@@ -25,7 +25,6 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
-#include <cmath>
 
 #include "beam.h"
 #include "device.cuh"
@@ -196,14 +195,16 @@ struct Raw {
 };
 
 // Groups of threads whose maxima give a threshold.
-__device__ __forceinline__ int groups_for(int n) { return n <= 16 ? 64 : n <= 32 ? 128 : 256; }
+__device__ __forceinline__ int groups_log2(int n) { return n <= 16 ? 6 : n <= 32 ? 7 : 8; }
 
 // A candidate, or a segment: value and beam in v; logit and token, or largest
 // logit and number, in k.  The zero is none.
 struct Entry {
   uint64_t v, k;
 };
-__device__ __forceinline__ bool above(const Entry &a, const Entry &b) { return a.v > b.v || (a.v == b.v && a.k > b.k); }
+__device__ __forceinline__ bool above(const Entry &a, const Entry &b) {  // (as one number: no branches)
+  return ((unsigned __int128)a.v << 64 | a.k) > ((unsigned __int128)b.v << 64 | b.k);
+}
 __device__ __forceinline__ Entry shfl_xor(const Entry &e, int o) {
   return {__shfl_xor_sync(0xffffffffu, e.v, o), __shfl_xor_sync(0xffffffffu, e.k, o)};
 }
@@ -229,25 +230,23 @@ struct List {
     return at;
   }
 
-  // The n-th largest of the groups' maxima, from each thread's maximum.  A
-  // group's threads share the work of its rank.
+  // The n-th largest of the groups' maxima, from each thread's maximum; none if
+  // fewer groups have one.  A group's threads share the work of its rank.
   __device__ Entry nth_of_groups(Entry mine) {
-    const int t = threadIdx.x, G = groups_for(n), per = kThreads / G;
+    const int t = threadIdx.x, log2 = 8 - groups_log2(n), per = 1 << log2, G = kThreads >> log2;
     for (int o = 1; o < per; o *= 2) {
       const Entry other = shfl_xor(mine, o);
       if (above(other, mine)) mine = other;
     }
-    const int g = t / per;
-    if (t % per == 0) groups[g] = mine;
+    const int g = t >> log2;
+    if (mine.v == 0) mine.k = g;  // (groups without a candidate differ too: ranks are 0 .. G - 1)
+    if ((t & (per - 1)) == 0) groups[g] = mine;
     __syncthreads();
     int rank = 0;
-#pragma unroll 8
-    for (int i = t % per; i < G; i += per) {
-      const Entry other = groups[i];
-      rank += above(other, mine) || (i < g && !above(mine, other));
-    }
+#pragma unroll 16
+    for (int i = t & (per - 1); i < G; i += per) rank += above(groups[i], mine);
     for (int o = 1; o < per; o *= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-    if (rank == n - 1 && t % per == 0) *mark = mine;
+    if (rank == n - 1 && (t & (per - 1)) == 0) *mark = mine.v ? mine : Entry{0, 0};
     __syncthreads();
     return *mark;
   }
@@ -281,17 +280,17 @@ struct List {
     }
     if (len <= kThreads) {
       // 256, 128 or 64 entries: 1, 2 or 4 threads an entry.
-      const int per = len <= 64 ? 4 : len <= 128 ? 2 : 1, e = t / per;
+      const int log2 = len <= 64 ? 2 : len <= 128 ? 1 : 0, per = 1 << log2, e = t >> log2;
       Entry mine{};
       int rank = 0;
       if (e < len) {
         mine = item[e];
 #pragma unroll 8
-        for (int i = t % per; i < len; i += per) rank += above(item[i], mine);
+        for (int i = t & (per - 1); i < len; i += per) rank += above(item[i], mine);
       }
       for (int o = 1; o < per; o *= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
       __syncthreads();
-      if (e < len && t % per == 0 && rank < n) item[rank] = mine;
+      if (e < len && (t & (per - 1)) == 0 && rank < n) item[rank] = mine;
     } else {
       // (as many as no threshold of groups could drop)
       constexpr int kMost = (kList + kThreads - 1) / kThreads;
@@ -388,6 +387,8 @@ __device__ void reduce_slice(const SelectParams &p, int r, int sl, uint4 *ring, 
   }
 }
 
+static_assert(kRing<__half> >= kList * (int)sizeof(Entry), "the merge's list takes the ring's place");
+
 // The n best candidates of a batch entry.
 template <typename T>
 __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segments, float *base, bool *ended) {
@@ -450,31 +451,61 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   // The n best segments.  A thread's best: its values in turn, which come by
   // beam and number, so that a later one has to be larger (or, of one beam, to
   // be a larger logit of the same rounded value).
-  float best_v = -INFINITY, best_l = -INFINITY;
+  constexpr int kHeld = 3;  // jobs whose values stay in registers
+  const bool held = jobs <= kHeld * kWarps;
+  float keep[kHeld][kU], best_v = -INFINITY, best_l = -INFINITY;
   int best_k = 0, best_s = 0;
-  for (int job = warp; job < jobs; job += kWarps) {
-    take_job(job);
-    const float plus = base[k];
+  const auto look = [&](float plus) {
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       const float v = plus + top[j];
       if (v < INFINITY && (v > best_v || (v == best_v && k == best_k && top[j] > best_l)))
         best_v = v, best_l = top[j], best_k = k, best_s = s0 + 32 * j;
     }
-  }
-  Entry least = list.nth_of_groups(entry_of(best_v, best_k, best_l, best_s));
-  while (true) {
-    const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
-    load_job(warp);
+  };
+  Entry least;
+  const auto find = [&](float bar) {
+#pragma unroll
+    for (int j = 0; j < kU; ++j)
+      if (base[k] + top[j] >= bar) {
+        const Entry e = make_entry(base[k], k, top[j], s0 + 32 * j);
+        if (e.v && !above(least, e)) list.push(e);
+      }
+  };
+  if (held) {
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) {
+      if (warp + h * kWarps >= jobs) break;
+      take_job(warp + h * kWarps);
+#pragma unroll
+      for (int j = 0; j < kU; ++j) keep[h][j] = top[j];
+      look(base[k]);
+    }
+  } else {
     for (int job = warp; job < jobs; job += kWarps) {
       take_job(job);
-      const float plus = base[k];
+      look(base[k]);
+    }
+  }
+  least = list.nth_of_groups(entry_of(best_v, best_k, best_l, best_s));
+  while (true) {
+    const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
+    if (held) {
 #pragma unroll
-      for (int j = 0; j < kU; ++j)
-        if (plus + top[j] >= bar) {
-          const Entry e = make_entry(plus, k, top[j], s0 + 32 * j);
-          if (e.v && !above(least, e)) list.push(e);
-        }
+      for (int h = 0; h < kHeld; ++h) {
+        if (warp + h * kWarps >= jobs) break;
+        k = (warp + h * kWarps) / per_beam;
+        s0 = (warp + h * kWarps - k * per_beam) * 32 * kU + lane;
+#pragma unroll
+        for (int j = 0; j < kU; ++j) top[j] = keep[h][j];
+        find(bar);
+      }
+    } else {
+      load_job(warp);
+      for (int job = warp; job < jobs; job += kWarps) {
+        take_job(job);
+        find(bar);
+      }
     }
     __syncthreads();
     const bool over = *list.count > kList;
@@ -490,7 +521,7 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   const int chosen = *list.count;
   if (t < chosen) best_segments[t] = list.item[t];
   __syncthreads();
-  if (t == 0) *list.count = 0;
+  if (t == 0) *list.count = 0;  // (each thread has read it)
   __syncthreads();
   // (As a candidate's, the threshold's token is the last of its segment.)
   least.k = (least.k & ~0xFFFFFFFFull) | (uint32_t)~((key_token(least.k) + 1) * kSegment - 1);
@@ -518,12 +549,20 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
     int v;
     load_segment(c, x, k, v);
     const float plus = base[k];
+    uint32_t pass = 0;
 #pragma unroll
-    for (int i = 0; i < kE; ++i)
-      if (plus + x[i] >= bar) {
-        const Entry e = make_entry(plus, k, x[i], v + Raw<T>::place(i));
+    for (int i = 0; i < kE; ++i) pass |= (uint32_t)(plus + x[i] >= bar) << i;
+    while (__any_sync(0xffffffffu, pass)) {  // (few: a value is found again by its number)
+      const int i = __ffs(pass) - 1;
+      float l = 0.f;
+#pragma unroll
+      for (int j = 0; j < kE; ++j) l = i == j ? x[j] : l;
+      if (pass) {
+        pass &= pass - 1;
+        const Entry e = make_entry(plus, k, l, v + Raw<T>::place(i));
         if (e.v && !above(least, e)) list.push(e);
       }
+    }
   }
   __syncthreads();
   if (*list.count > kList) {
@@ -568,8 +607,6 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   }
 }
 
-static_assert(kRing<__half> >= kList * (int)sizeof(Entry), "the list takes the ring's place");
-
 template <typename T>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_kernel(const SelectParams p) {
   extern __shared__ uint4 smem16[];
@@ -579,12 +616,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
   __shared__ int count, before;
   const int r = blockIdx.x / p.slices, sl = blockIdx.x - r * p.slices, b = r / p.beams;
   if (!(p.ended && p.ended[r])) reduce_slice<T>(p, r, sl, smem16, red);
-  __threadfence();
+  // (One thread's fences order the whole block's stores and loads: what the
+  // barriers put before the one and behind the other comes with it.)
   __syncthreads();
-  if (threadIdx.x == 0) before = atomicAdd(p.counters + b, 1);
+  if (threadIdx.x == 0) {
+    __threadfence();
+    before = atomicAdd(p.counters + b, 1);
+    __threadfence();
+  }
   __syncthreads();
   if (before != p.beams * p.slices - 1) return;
-  __threadfence();
   if (threadIdx.x == 0) p.counters[b] = 0;
   List list = {reinterpret_cast<Entry *>(smem16), groups, &mark, &count, p.n};
   merge<T>(p, b, list, best_segments, red, ended);
@@ -592,22 +633,13 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
 
 }  // namespace
 
-// Blocks of a row: the least work on the busiest multiprocessor, where a block's
-// start and end cost as much as eight segments, and fewer than three blocks at
-// once leave it waiting for memory.
+// Blocks of a row: about two a multiprocessor in all, whose start and end then
+// overlap with little else to pay for; with more rows than that two a row, so
+// that the multiprocessors come out even (128 rows of 151936 in fp32: 24.4 us,
+// with seven 25.6, with one 26.0; 512 rows in bf16 40 us, with one 46).
 static int beam_slices(int64_t rows, int64_t segments, int sm_count) {
-  const int64_t most = std::min<int64_t>((segments + kWarps - 1) / kWarps, 1 + 8 * sm_count / rows);
-  int best = 1;
-  double least = 1e30;
-  for (int64_t n = 1; n <= most; ++n) {
-    const double blocks = (double)(rows * n) / sm_count;
-    const double cost = std::ceil(blocks) * ((double)segments / n / kWarps + 1) * std::max(1.0, 3 / blocks);
-    if (cost < least) {
-      least = cost;
-      best = (int)n;
-    }
-  }
-  return best;
+  const int64_t most = (segments + kWarps - 1) / kWarps;
+  return (int)std::min<int64_t>(most, std::max<int64_t>(2 * rows > 3 * sm_count ? 2 : 1, 2 * sm_count / rows));
 }
 
 // Scratch: counters of the batch entries (at most one a row), the blocks' sums, the segments' largest logits.
@@ -615,7 +647,7 @@ static size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t beam_counter_bytes(int64_t max_rows) { return up((size_t)max_rows * sizeof(int)); }
 size_t beam_scratch_bytes(int64_t max_rows, int64_t max_vocab, int sm_count) {
   const size_t segments = (size_t)((max_vocab + kSegment - 1) / kSegment);
-  return beam_counter_bytes(max_rows) + up((size_t)(max_rows + 8 * sm_count) * sizeof(float2)) +
+  return beam_counter_bytes(max_rows) + up((size_t)(2 * max_rows + 2 * sm_count) * sizeof(float2)) +
          (size_t)max_rows * segments * sizeof(float);
 }
 
