@@ -11,10 +11,14 @@
 //   - finds the n best segments by their largest values: no other holds one of
 //     the n best candidates;
 //   - reads those again and takes the n best candidates of them.
-// Both searches go by a threshold first: of the maxima of G groups of threads
-// the n-th largest is no more than the n-th largest of all, and with G = 4 n it
-// is passed by about 1.15 n.  Candidates compare by value, beam, logit and token
-// (segments by their number), so there are no ties and what passes is bounded.
+// Both searches go by a threshold first, which n entries reach for certain and
+// few more: for the segments one from the threads' largest values, for the
+// candidates the n-th best segment's.  Entries compare by value, beam, logit and
+// token (segments by their number), so there are no ties.  Where more pass than
+// the list takes (equal values, a segment that holds most of the best) the
+// search is made again with a threshold that bounds what passes: of the maxima
+// of G groups of threads the n-th largest is no more than the n-th of all, and
+// no more than n groups hold what reaches it.
 //
 // (Keeping a list of the n best in every block cost more than the reading: lists
 // with a threshold that all warps share met at a barrier for every tile, lists
@@ -208,12 +212,10 @@ __device__ __forceinline__ bool above(const Entry &a, const Entry &b) {  // (as 
 __device__ __forceinline__ Entry shfl_xor(const Entry &e, int o) {
   return {__shfl_xor_sync(0xffffffffu, e.v, o), __shfl_xor_sync(0xffffffffu, e.k, o)};
 }
-__device__ __forceinline__ Entry entry_of(float v, int beam, float logit, uint32_t number) {
+__device__ __forceinline__ Entry make_entry(float base, int beam, float logit, uint32_t number) {
+  const float v = base + logit;
   if (!isfinite(v)) return {0, 0};
   return {(uint64_t)ordered(v) << 32 | (uint32_t)~beam, make_key(logit, number)};
-}
-__device__ __forceinline__ Entry make_entry(float base, int beam, float logit, uint32_t number) {
-  return entry_of(base + logit, beam, logit, number);
 }
 
 // The best entries seen, in shared memory.
@@ -313,6 +315,28 @@ struct List {
     return len >= n ? item[n - 1] : Entry{0, 0};
   }
 };
+
+// A value that n of the threads' values (ordered, 0: none) reach, at most twice as
+// many as that or so: the least of the warps' k-th largest, with 8 k >= n, the
+// values dealt out evenly.  0: fewer have one.
+__device__ __forceinline__ uint32_t reached_by(int n, uint32_t mine, uint32_t *shared) {
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  shared[t] = mine;
+  __syncthreads();
+  mine = shared[lane * kWarps + warp];
+  uint32_t kth = 0;
+  for (int k = 0; k < n; k += kWarps) {
+    kth = __reduce_max_sync(0xffffffffu, mine);
+    if (__ffs(__ballot_sync(0xffffffffu, mine == kth)) - 1 == lane) mine = 0;
+  }
+  __syncthreads();
+  if (lane == 0) shared[warp] = kth;
+  __syncthreads();
+  uint32_t least = shared[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) least = min(least, shared[w]);
+  return least;
+}
 
 __device__ __forceinline__ float warp_max_f(float v) {
 #pragma unroll
@@ -448,19 +472,15 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   if (t == 0) *list.count = 0;
   __syncthreads();
 
-  // The n best segments.  A thread's best: its values in turn, which come by
-  // beam and number, so that a later one has to be larger (or, of one beam, to
-  // be a larger logit of the same rounded value).
+  // The n best segments, of those whose value reaches a first threshold.
   constexpr int kHeld = 3;  // jobs whose values stay in registers
   const bool held = jobs <= kHeld * kWarps;
-  float keep[kHeld][kU], best_v = -INFINITY, best_l = -INFINITY;
-  int best_k = 0, best_s = 0;
+  float keep[kHeld][kU], best_v = -INFINITY;
   const auto look = [&](float plus) {
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       const float v = plus + top[j];
-      if (v < INFINITY && (v > best_v || (v == best_v && k == best_k && top[j] > best_l)))
-        best_v = v, best_l = top[j], best_k = k, best_s = s0 + 32 * j;
+      if (v < INFINITY) best_v = fmaxf(best_v, v);
     }
   };
   Entry least;
@@ -487,7 +507,9 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
       look(base[k]);
     }
   }
-  least = list.nth_of_groups(entry_of(best_v, best_k, best_l, best_s));
+  least = {(uint64_t)reached_by(p.n, best_v > -INFINITY ? ordered(best_v) : 0, reinterpret_cast<uint32_t *>(list.groups))
+               << 32,
+           0};
   while (true) {
     const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
     if (held) {
@@ -525,29 +547,37 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
   __syncthreads();
   // (As a candidate's, the threshold's token is the last of its segment.)
   least.k = (least.k & ~0xFFFFFFFFull) | (uint32_t)~((key_token(least.k) + 1) * kSegment - 1);
-  // This lane's logits of the c-th segment, of beam k and from token v (an ended beam: a logit of 0 in place 0).
-  const auto load_segment = [&](int c, float(&x)[kE], int &beam, int &v) {
-#pragma unroll
-    for (int i = 0; i < kE; ++i) x[i] = -INFINITY;
+  // This lane's logits of the c-th segment, of a beam and from token v (an ended
+  // beam: a logit of 0 in place 0).
+  const auto load_segment = [&](int c, Raw<T> &raw, int &beam, int &v) {
     beam = v = 0;
     if (c >= chosen) return;
     const Entry seg = best_segments[c];
     beam = (int)~(uint32_t)seg.v;
-    if (ended[beam]) {
-      if (lane == 0) x[0] = 0.f;
-    } else {
-      v = (int)key_token(seg.k) * kSegment;
-      Raw<T> raw;
-      raw.load(static_cast<const T *>(p.logits) + (int64_t)(r0 + beam) * p.ld, v, p.vocab, p.vec);
+    v = (int)key_token(seg.k) * kSegment;
+    if (!ended[beam]) raw.load(static_cast<const T *>(p.logits) + (int64_t)(r0 + beam) * p.ld, v, p.vocab, p.vec);
+  };
+  const auto values_of = [&](int c, const Raw<T> &raw, int beam, float(&x)[kE]) {
+    if (c < chosen && !ended[beam]) {
       raw.values(x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kE; ++i) x[i] = -INFINITY;
+      if (c < chosen && lane == 0) x[0] = 0.f;
     }
   };
-  // The candidates that reach the threshold, straight away: about as many as there are segments.
+  // The candidates that reach the threshold, straight away: about as many as
+  // there are segments.  The next segment's loads are under way.
   const float bar = least.v ? unordered((uint32_t)(least.v >> 32)) : -INFINITY;
+  Raw<T> ahead;
+  int next_k, next_v;
+  load_segment(warp, ahead, next_k, next_v);
   for (int c = warp; c < chosen; c += kWarps) {
     float x[kE];
-    int v;
-    load_segment(c, x, k, v);
+    k = next_k;
+    const int v = next_v;
+    values_of(c, ahead, k, x);
+    load_segment(c + kWarps, ahead, next_k, next_v);
     const float plus = base[k];
     uint32_t pass = 0;
 #pragma unroll
@@ -573,7 +603,8 @@ __device__ void merge(const SelectParams &p, int b, List &list, Entry *best_segm
     for (int c = 0; c < chosen; c += kWarps) {
       float x[kE];
       int v;
-      load_segment(c + warp, x, k, v);
+      load_segment(c + warp, ahead, k, v);
+      values_of(c + warp, ahead, k, x);
       const float plus = base[k];
       Entry top_entry = {0, 0};
 #pragma unroll
@@ -633,13 +664,17 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
 
 }  // namespace
 
-// Blocks of a row: about two a multiprocessor in all, whose start and end then
-// overlap with little else to pay for; with more rows than that two a row, so
-// that the multiprocessors come out even (128 rows of 151936 in fp32: 24.4 us,
-// with seven 25.6, with one 26.0; 512 rows in bf16 40 us, with one 46).
+// Blocks of a row: about two a multiprocessor in all, whose starts and ends then
+// overlap, and no fewer than one and a half (128 rows of 151936 in fp32: two
+// 24.4 us, seven 25.6, one 26.0; 160 rows of which 64 have ended, 262144 in bf16:
+// seven 25.7 us, one 34.7); with more rows than multiprocessors take, two a row,
+// so that these come out even (512 rows in bf16 40 us, with one 46).
 static int beam_slices(int64_t rows, int64_t segments, int sm_count) {
   const int64_t most = (segments + kWarps - 1) / kWarps;
-  return (int)std::min<int64_t>(most, std::max<int64_t>(2 * rows > 3 * sm_count ? 2 : 1, 2 * sm_count / rows));
+  int64_t n = 2 * sm_count / rows;
+  if (2 * rows * n < 3 * sm_count) ++n;
+  if (2 * rows > 3 * sm_count) n = 2;
+  return (int)std::min(most, n);
 }
 
 // Scratch: counters of the batch entries (at most one a row), the blocks' sums, the segments' largest logits.
@@ -647,7 +682,7 @@ static size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t beam_counter_bytes(int64_t max_rows) { return up((size_t)max_rows * sizeof(int)); }
 size_t beam_scratch_bytes(int64_t max_rows, int64_t max_vocab, int sm_count) {
   const size_t segments = (size_t)((max_vocab + kSegment - 1) / kSegment);
-  return beam_counter_bytes(max_rows) + up((size_t)(2 * max_rows + 2 * sm_count) * sizeof(float2)) +
+  return beam_counter_bytes(max_rows) + up((size_t)(2 * max_rows + 4 * sm_count) * sizeof(float2)) +
          (size_t)max_rows * segments * sizeof(float);
 }
 
