@@ -154,25 +154,33 @@ __global__ void __launch_bounds__(kThreads, 1) int8_decode_kernel(const I8Decode
   } else {
     if (threadIdx.x < 8 * kTiles) s_scale[threadIdx.x] = threadIdx.x < p.M ? p.x_scales[threadIdx.x] : 0.f;
     if constexpr (kSource == kFromCodes) {
-      const int8_t *x = static_cast<const int8_t *>(p.x);
-      if (p.vec) {  // whole rows of 16 bytes
-        const int per = p.K_pad / 16;
+      // Several warps a row where there are few rows.
+      int per = kWarps;
+      while (per > 1 && per * p.M > kWarps) per /= 2;
+      for (int m = warp / per; m < p.M; m += kWarps / per) {
+        const int8_t *row = static_cast<const int8_t *>(p.x) + m * p.ldx;
+        int8_t *to = xs + m * pitch;
+        if (p.vec) {  // (whole rows of 16 bytes)
 #pragma unroll 4
-        for (int i = threadIdx.x; i < p.M * per; i += 32 * kWarps) {
-          const int m = i / per, c = i - m * per;
-          *reinterpret_cast<uint4 *>(xs + m * pitch + 16 * c) =
-              16 * c < p.K ? *reinterpret_cast<const uint4 *>(x + m * p.ldx + 16 * c) : make_uint4(0, 0, 0, 0);
-        }
-      } else {
-        const int per = p.K_pad / 4;
+          for (int k = 16 * (warp % per * 32 + lane); k < p.K_pad; k += 512 * per)
+            *reinterpret_cast<uint4 *>(to + k) =
+                k < p.K ? *reinterpret_cast<const uint4 *>(row + k) : make_uint4(0, 0, 0, 0);
+        } else {
+          // A row may start on any byte: its codes come out of the aligned words they lie in.
+          const int shift = 8 * (int)(reinterpret_cast<uintptr_t>(row) & 3), second = shift > 0;
+          const uint32_t *words = reinterpret_cast<const uint32_t *>(row - shift / 8);
+          const int k0 = 4 * (warp % per * 32 + lane);
 #pragma unroll 4
-        for (int i = threadIdx.x; i < p.M * per; i += 32 * kWarps) {
-          const int m = i / per, k = 4 * (i - m * per);
-          const int8_t *row = x + m * p.ldx;
-          int c[4];
+          for (int k = k0; k + 8 <= p.K; k += 128 * per)
+            *reinterpret_cast<uint32_t *>(to + k) = __funnelshift_r(words[k / 4], words[k / 4 + second], shift);
+          // The last ones, whose second word may lie past the row, by bytes; then zeros.
+          for (int k = k0 + (p.K - k0 < 8 ? 0 : (p.K - k0 - 8) / (128 * per) + 1) * (128 * per); k < p.K_pad; k += 128 * per) {
+            uint32_t v = 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) c[j] = k + j < p.K ? row[k + j] : 0;
-          *reinterpret_cast<uint32_t *>(xs + m * pitch + k) = pack_bytes(c[0], c[1], c[2], c[3]);
+            for (int j = 0; j < 4; ++j)
+              if (k + j < p.K) v |= (uint32_t)(uint8_t)row[k + j] << (8 * j);
+            *reinterpret_cast<uint32_t *>(to + k) = v;
+          }
         }
       }
     }

@@ -66,51 +66,65 @@ __device__ __forceinline__ void load8(const T *p, bool vec, int64_t left, float 
   r.values(v);
 }
 
-// Bits of the largest |v|: they are ordered as the values are, infinities and NaNs above all others.
-__device__ __forceinline__ uint32_t abs_max8(const float (&v)[8], uint32_t mx) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) mx = max(mx, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return mx;
+// A running maximum of |v| whose NaNs stay; its bits order as the values do, a
+// NaN above infinity.
+__device__ __forceinline__ float abs_max(float a, float b) {
+  asm("max.NaN.xorsign.abs.f32 %0, %0, %1;\n" : "+f"(a) : "f"(b));  // (the sign is of no account)
+  return a;
+}
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// The largest |value| of eight as abs_bits; 16-bit types compare as integers, two at once.
+template <typename T>
+__device__ __forceinline__ uint32_t abs_max8(const Raw8<T> &raw) {
+  if constexpr (sizeof(T) == 4) {
+    float v[8];
+    raw.values(v);
+    float m = abs_max(abs_max(abs_max(v[0], v[1]), abs_max(v[2], v[3])), abs_max(abs_max(v[4], v[5]), abs_max(v[6], v[7])));
+    return abs_bits(m);
+  } else {
+    constexpr uint32_t kAbs = 0x7FFF7FFFu;
+    const uint32_t m = __vmaxu2(__vmaxu2(raw.r[0].x & kAbs, raw.r[0].y & kAbs), __vmaxu2(raw.r[0].z & kAbs, raw.r[0].w & kAbs));
+    const uint16_t h = max((uint16_t)m, (uint16_t)(m >> 16));
+    return abs_bits(to_f32(*reinterpret_cast<const T *>(&h)));
+  }
 }
 
 __device__ __forceinline__ float token_scale(uint32_t max_bits) { return __fdiv_rn(__uint_as_float(max_bits), 127.f); }
 
-// A row's quantiser.  Bit for bit the definition, without a division for each
-// value: adding 1.5 * 2^23 in the FMA rounds v * inv (inv = 1 / scale, rounded)
-// to an integer n, ties to even, in the sum's low bits.  v * inv and the
-// rounded quotient differ by less than 2^-22 of their size, below 4e-5 for
-// |v / scale| < 128, so unless v * inv lies within 1e-4 of a half-integer both
-// round to n (about 1 value in 5000 does).  Those, and rows whose scale is
-// outside [2^-100, 2^100] (whose reciprocal may not be that near, or whose
-// quotients may pass 127), take the definition.
+// A row's quantiser: bit for bit the definition, without a division for each
+// value.  With inv the correctly rounded reciprocal of the scale s, q0 = v inv
+// is within an ulp of v / s, r = v - q0 s is exact in an FMA, and q0 + r inv,
+// rounded once, is v / s correctly rounded (P. Markstein, "Computation of
+// elementary functions on the IBM RISC System/6000 processor", 1990).  Adding 1.5 *
+// 2^23 rounds it to an integer, ties to even, in the sum's low bits.  Rows whose scale
+// is outside [2^-80, 2^100] (residuals may underflow, quotients may pass 127)
+// are divided.
 struct TokenQuantizer {
   float s, inv;
   bool fast, zero;
   __device__ __forceinline__ explicit TokenQuantizer(float scale) : s(scale) {
     zero = !(s > 0.f) || isinf(s);
-    fast = s >= 7.88860905e-31f && s <= 1.26765060e30f;
+    fast = s >= 8.27180613e-25f && s <= 1.26765060e30f;
     inv = fast ? __frcp_rn(s) : 0.f;
   }
   __device__ __forceinline__ int slow(float v) const {
     return zero ? 0 : (int)fminf(fmaxf(rintf(__fdiv_rn(v, s)), -127.f), 127.f);
   }
-  // A code is the low byte of what these give.
-  __device__ __forceinline__ int code(float v) const {
-    constexpr float kMagic = 12582912.f;
-    const float t = fmaf(v, inv, kMagic);
-    if (!fast || fabsf(fmaf(v, inv, -(t - kMagic))) > 0.4999f) return slow(v);
-    return __float_as_int(t);
+  // Two codes as the low bytes of c0 and c1.
+  __device__ __forceinline__ void codes2(float v0, float v1, int &c0, int &c1) const {
+    const float2 v = make_float2(v0, v1), i = make_float2(inv, inv);
+    const float2 q0 = __fmul2_rn(v, i);
+    const float2 r = __ffma2_rn(make_float2(-q0.x, -q0.y), make_float2(s, s), v);
+    const float2 n = __fadd2_rn(__ffma2_rn(r, i, q0), make_float2(12582912.f, 12582912.f));
+    c0 = __float_as_int(n.x);
+    c1 = __float_as_int(n.y);
   }
   __device__ __forceinline__ void codes8(const float (&v)[8], int (&c)[8]) const {
-    constexpr float kMagic = 12582912.f;
-    float off = 0.f;
+    if (fast) {  // (the same for a whole row)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = fmaf(v[i], inv, kMagic);
-      c[i] = __float_as_int(t);
-      off = fmaxf(off, fabsf(fmaf(v[i], inv, -(t - kMagic))));  // distance from n
-    }
-    if (!fast || off > 0.4999f) {
+      for (int i = 0; i < 8; i += 2) codes2(v[i], v[i + 1], c[i], c[i + 1]);
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] = slow(v[i]);
     }
@@ -145,10 +159,7 @@ __device__ __forceinline__ void quantize_to_shared(const T *x, int64_t ldx, int 
 #pragma unroll
         for (int u = 0; u < kU; ++u) raw[u].load(row + base + u * stride, vec, K - (base + u * stride));
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          raw[u].values(v);
-          mx = abs_max8(v, mx);
-        }
+        for (int u = 0; u < kU; ++u) mx = max(mx, abs_max8(raw[u]));
       }
       mx = __reduce_max_sync(0xffffffffu, mx);
     }
