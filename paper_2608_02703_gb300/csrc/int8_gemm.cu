@@ -15,8 +15,10 @@
 //     stores them as the A operand in tensor memory, whose tcgen05.st.16x128b
 //     registers are the fragment registers that the words hold;
 //   - one thread issues eight MMAs into a TMEM accumulator that holds the whole
-//     K of the unit;
-//   - epilogue warps read the accumulator, scale, round and store.
+//     K of the unit; up to 128 tokens a unit two threads take stages in turn, each
+//     with an accumulator of its own (a thread needs some 700 cycles for a stage's
+//     eight MMAs, which run 312 for 64 tokens and 536 for 128);
+//   - epilogue warps read the accumulators, scale, round and store.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -40,14 +42,15 @@ struct I8Geom {
   static constexpr int kConv = NT == 256 ? 2 : NT == 128 && kSplit ? 3 : 4;  // converter warpgroups
   static constexpr int kXS = NT == 64 ? (kSplit ? 4 : 6) : NT == 128 ? (kSplit ? 3 : 4) : 2;
   static constexpr int kA = kOne ? kXS : 4;        // A stages
-  static constexpr int kAcc = NT == 64 ? 2 : 256 / NT;
+  static constexpr int kIssue = kOne && kXS % 2 == 0 ? 2 : 1;  // issuing threads (see there)
+  static constexpr int kAcc = (kPfTmemCols - kA * 64) / (NT * kIssue);  // units whose accumulators there are
   static constexpr int kEpi = NT == 64 ? 1 : 2;    // epilogue warpgroups
   static constexpr int kCols = NT / kEpi;          // accumulator columns a thread takes
   static constexpr int kThreads = 128 * (1 + kConv + kEpi);
   static constexpr int kBoxBytes = NT * 64 * 2;
   static constexpr int kXBytes = 2 * kBoxBytes;
   static constexpr int kCodeSlot = kI8PadN * kI8PadK;  // 16 KB
-  static constexpr int kCS = NT == 64 ? 7 : NT == 128 && kSplit ? 4 : 5;
+  static constexpr int kCS = NT == 64 ? 8 : NT == 128 ? (kSplit ? 4 : 6) : 5;
   static constexpr int kCodeOff = kXS * kXBytes;
   static constexpr int kJoinOff = kCodeOff + kCS * kCodeSlot;  // sums of this block's tokens, from every block of the cluster
   static constexpr int kJoinBytes = kSplit ? NT * kI8PadN * 4 : 0;
@@ -58,9 +61,10 @@ struct I8Geom {
   static constexpr int kRegsC = NT == 64 || kConv == 3 ? 72 : 56;
   static constexpr int kRegsP = NT == 64 ? 128 : NT == 128 ? (kSplit ? 104 : 112) : 160;
   static_assert(128 * (kRegs0 + kConv * kRegsC + kEpi * kRegsP) <= 65536 / kThreads / 8 * 8 * kThreads, "registers");
-  static_assert(kAcc * NT + kA * 64 <= kPfTmemCols, "TMEM columns");
+  static_assert(kAcc * kIssue * NT + kA * 64 <= kPfTmemCols, "TMEM columns");
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kA >= kConv && kCS >= kA, "stages and slots (see the converters)");
+  static_assert(kIssue == 1 || (kA % 2 == 0 && kConv % 2 == 0 && kCS % 2 == 0), "stages of two issuers (see the converters)");
 };
 
 struct I8GemmParams {
@@ -154,8 +158,8 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     for (int i = 0; i < kXS && !G::kOne; ++i) mbar_init(&x_full[i], 1), mbar_init(&x_empty[i], 1);
     for (int i = 0; i < kCS; ++i) mbar_init(&c_full[i], 1), mbar_init(&c_empty[i], 4);
     for (int i = 0; i < kA; ++i) mbar_init(&a_full[i], G::kOne ? 5 : 4), mbar_init(&a_empty[i], 1);
-    for (int i = 0; i < kAcc; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 4 * G::kEpi);
-    mbar_init(drain, 1);
+    for (int i = 0; i < kAcc; ++i) mbar_init(&acc_full[i], G::kIssue), mbar_init(&acc_empty[i], 4 * G::kEpi);
+    mbar_init(drain, G::kIssue);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -164,7 +168,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const uint32_t a_base = tmem_base + kAcc * NT;
+  const uint32_t a_base = tmem_base + kAcc * G::kIssue * NT;
   bool mma_leader = false;
 
   // Unit u: tokens u % num_mt of tile u / num_mt.  With kSplit a cluster has one
@@ -222,7 +226,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
           __syncwarp();
         }
       }
-    } else if (warp == 1) {
+    } else if (warp == 1 || (warp == 3 && G::kIssue == 2)) {
       // ------------------------------ MMAs ------------------------------
       const bool leader = elect_one();
       mma_leader = leader;
@@ -232,11 +236,24 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       RingPos<kXS> xr;
       RingPos<kA> ar;
       RingPos<kAcc> accr;
+      // Of two issuing threads each takes every other stage, counted over all
+      // units: with an even number of stages in the ring a stage's place is then
+      // always the same thread's, and it has seen that place's last phase.
+      const int me = warp >> 1;
+      int turn = 0;
       bool polled = false;  // the next stage's barrier was seen complete
       for (int u = u0; u < p.units; u += step) {
         if (!mbar_wait_warp(&acc_empty[accr.s], accr.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
-        const uint32_t d = tmem_base + accr.s * NT;
+        const uint32_t d = tmem_base + (accr.s * G::kIssue + (G::kIssue == 2 ? me : 0)) * NT;
+        bool first = true;
         for (int e = begin; e < end; ++e) {
+          const bool mine = G::kIssue == 1 || turn == me;
+          turn ^= 1;
+          if (!mine) {
+            xr.next();
+            ar.next();
+            continue;
+          }
           if (!G::kOne && !mbar_wait_warp(&x_full[xr.s], xr.ph, p.wait_budget, abort_flag, p.err)) goto done;
           if (!__all_sync(0xffffffffu, polled) &&
               !mbar_wait_warp(&a_full[ar.s], ar.ph, p.wait_budget, abort_flag, p.err))
@@ -244,25 +261,27 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
           tc_fence_after();
           const uint32_t a = a_base + ar.s * 64;
           const uint64_t b = xdesc + (uint32_t)((G::kOne ? ar.s : xr.s) * (G::kXBytes >> 4));
-          const RingPos<kA> now = ar;
+          const RingPos<kA> now = ar, ahead = ar.ahead(G::kIssue);
           ar.next();
           if (leader) {
 #pragma unroll
             for (int q = 0; q < 4; ++q)  // (+2 in the descriptor: 32 bytes)
-              tc_mma_ts(d, a + 8 * q, b + 2 * q, idesc, q > 0 || e > begin);
+              tc_mma_ts(d, a + 8 * q, b + 2 * q, idesc, q > 0 || !first);
           }
+          first = false;
           __syncwarp();
-          polled = mbar_test_a(smem_u32(&a_full[ar.s]), ar.ph);  // (under way while the others are issued)
+          polled = mbar_test_a(smem_u32(&a_full[ahead.s]), ahead.ph);  // (under way while the others are issued)
           if (leader) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) tc_mma_ts(d, a + 8 * (q + 4), b + kBox + 2 * q, idesc, 1);
             if (!G::kOne) tc_commit(&x_empty[xr.s]);
             tc_commit(&a_empty[now.s]);
-            if (e + 1 == end) tc_commit(&acc_full[accr.s]);
           }
           __syncwarp();
           xr.next();
         }
+        if (leader) tc_commit(&acc_full[accr.s]);  // (of all this thread's MMAs, if it had any)
+        __syncwarp();
         accr.next();
       }
     }
@@ -281,9 +300,13 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
         // A parity shows only one phase from the next, so a barrier may be at most
         // one behind what is waited for.  The A stage's: this warpgroup's last
         // stage n - kConv waited for the MMAs of n - kConv - kA, which with kA >=
-        // kConv are behind those that used this stage before the last.  Then the
-        // code slot's: that the A stage is free says that all stages up to n -
-        // kA are converted, so kCS >= kA.
+        // kConv are behind those that used this place before the last.  Then the
+        // code slot's: that the A stage is free says that the MMAs of n - kA are
+        // done, so with kCS >= kA those of n - kCS are, and its codes had come.
+        // Both hold for the MMAs of one thread, which end in order.  Of two
+        // threads those of stages an even number apart do: kConv, kA and kCS are
+        // even then.  (With five code slots a converter could pass a barrier whose
+        // copy, from DRAM out of order, had not come.)
         if (!mbar_wait_warp(&a_empty[ar.s], ar.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
         if (!mbar_wait_warp(&c_full[cr.s], cr.ph, p.wait_budget, abort_flag, p.err)) goto done;
         tc_fence_after();
@@ -326,6 +349,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     const int col0 = kCols * pw;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(lg * 32) << 16) + col0;
     RingPos<kAcc> accr;
+    int stages = 0;  // of the units before, modulo 2
     asm volatile("griddepcontrol.wait;\n" ::: "memory");  // (the tokens' scales)
     for (int u = u0; u < p.units; u += step) {
       const int64_t n = (int64_t)(u / p.num_mt) * kI8PadN + lg * 32 + lane;
@@ -339,14 +363,28 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       if (!mbar_wait_warp(&acc_full[accr.s], accr.ph, p.wait_budget, abort_flag, p.err)) goto done;
       tc_fence_after();
       float acc[kCols];
+      // The first accumulator: of two that of the thread that had the unit's first stage.
+      const uint32_t acc0 = lane_addr + (accr.s * G::kIssue + (G::kIssue == 2 ? stages : 0)) * NT;
 #pragma unroll
       for (int c = 0; c < kCols; c += 16) {
         uint32_t v[16];
-        tmem_ld16<false>(lane_addr + accr.s * NT + c, v);
+        tmem_ld16<false>(acc0 + c, v);
         tmem_wait_ld(v);
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[c + i] = __uint_as_float(v[i]);
       }
+      if (G::kIssue == 2 && end - begin > 1) {
+        const uint32_t acc1 = lane_addr + (accr.s * 2 + (stages ^ 1)) * NT;
+#pragma unroll
+        for (int c = 0; c < kCols; c += 16) {
+          uint32_t v[16];
+          tmem_ld16<false>(acc1 + c, v);
+          tmem_wait_ld(v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c + i] += __uint_as_float(v[i]);
+        }
+      }
+      stages ^= (end - begin) & 1;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[accr.s]);
@@ -397,8 +435,8 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     }
   }
 done:
-  if (warp == 1 && mma_leader) {
-    tc_commit(drain);
+  if (mma_leader) {
+    tc_commit(drain);  // (each issuing thread's)
     mbar_wait(drain, 0, p.wait_budget, nullptr, p.err);
   }
   if (kSplit && !at_barrier) {  // every thread meets its cluster once, whatever became of its work

@@ -173,6 +173,28 @@ def test_product_split_and_whole(M, N, K, path):
     w.close()
 
 
+@pytest.mark.parametrize("M", [1, 8, 20, 40, 64, 100, 128, 200, 300])
+def test_wide_weights_from_memory(M):
+    """Many units a block, whose codes come from memory (more of them than the second-level cache holds) and so in any
+    order; repeated."""
+    torch = _torch()
+    N, K = 70000, 2304
+    g = torch.Generator(device="cuda").manual_seed(M)
+    codes = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    x = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    w = archead.archead_int8_weight_create(codes, torch.ones(N, device="cuda"))
+    # Sums below 2^24 are exact: 64-bit products of the codes, rows at a time.
+    want = torch.cat([x.double() @ codes[n:n + 10000].double().t() for n in range(0, N, 10000)], dim=1)
+    assert float(want.abs().max()) < 2 ** 24
+    y = torch.empty((M, N), device="cuda")
+    for _ in range(6):
+        y.fill_(float("nan"))
+        archead.archead_int8_matmul(w, x, torch.ones(M, device="cuda"), M, y)
+        assert archead.archead_int8_sync_status(w) == archead.OK
+        assert torch.equal(y.double(), want)
+    w.close()
+
+
 @pytest.mark.parametrize("path", list(PATHS))
 @pytest.mark.parametrize("M,K", [(3, 131071), (20, 40000), (70, 20000), (140, 5000)], ids=str)
 def test_largest_sums(M, K, path):
