@@ -40,14 +40,19 @@ size_t beam_counter_bytes(int64_t max_rows);
 
 cudaError_t launch_beam_select(SelectParams p, int dtype, void *ws, int64_t max_rows, int sm_count, cudaStream_t s);
 
+// Division of numbers below 2^31 by a constant d: q = (n m) >> (31 + l), with l =
+// ceil(log2 d) and m = floor(2^(31 + l) / d) + 1 < 2^32 (m = 0: d is 1).
+struct Divisor {
+  uint32_t d, m, shift;
+};
+
 constexpr int kReorderStates = 48;  // states of one launch
 struct ReorderState {
   const char *src;
   char *dst;
   int64_t outer_stride, row_stride, inner_stride;
-  int64_t total;       // vectors of one row
-  int64_t chunk;       // vectors of a chunk
-  int inner;
+  uint32_t total;      // vectors of one row, below 2^31
+  Divisor chunk, per;  // vectors of a chunk, of all inner chunks
   int width;           // bytes of a vector
   int first_tile;      // tiles of the states before this one
 };
@@ -59,6 +64,6 @@ struct ReorderParams {
 };
 cudaError_t launch_beam_reorder(const ReorderParams &p, cudaStream_t s);
 int reorder_vector_bytes(int beams);  // most bytes a thread moves of each row
-constexpr int kReorderTile = 256;     // vectors of a row that a block moves
+int reorder_tile();                   // vectors of a row that a block moves
 
 }  // namespace archead

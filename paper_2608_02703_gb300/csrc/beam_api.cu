@@ -12,6 +12,64 @@ namespace {
 // The largest power of two up to 16 that divides v.
 int64_t low_bits(int64_t v) { return v == 0 ? 16 : std::min<int64_t>(v & -v, 16); }
 
+Divisor divisor(uint32_t d) {
+  if (d == 1) return {1, 0, 0};
+  uint32_t l = 0;
+  while (((uint64_t)1 << l) < d) ++l;
+  return {d, (uint32_t)(((uint64_t)1 << (31 + l)) / d + 1), l - 1};
+}
+
+// Launches of a reordering, filled state by state.  In place and into another
+// buffer are launches of their own.
+struct Reordering {
+  ReorderParams p;
+  int64_t tiles = 0;
+  cudaStream_t stream;
+  cudaError_t failed = cudaSuccess;
+
+  void flush() {
+    if (p.count > 0 && failed == cudaSuccess) {
+      p.tiles = (int)tiles;
+      failed = launch_beam_reorder(p, stream);
+    }
+    p.count = 0;
+    tiles = 0;
+  }
+
+  // `bytes` of each of outer x inner chunks; states whose vectors of a row pass
+  // 2^31 in parts.
+  void add(const char *src, char *dst, int64_t outer, int64_t inner, int64_t bytes, const archead_beam_state &a,
+           int64_t width) {
+    const int64_t chunk = bytes / width;
+    if ((__int128)outer * inner * chunk >= (int64_t)1 << 31) {
+      const auto both = [&](int64_t step, int64_t o0, int64_t i0, int64_t b0, int64_t o1, int64_t i1, int64_t b1) {
+        add(src, dst, o0, i0, b0, a, width);
+        add(src + step, dst + step, o1, i1, b1, a, width);
+      };
+      if (outer > 1) return both(outer / 2 * a.outer_stride, outer / 2, inner, bytes, outer - outer / 2, inner, bytes);
+      if (inner > 1) return both(inner / 2 * a.inner_stride, 1, inner / 2, bytes, 1, inner - inner / 2, bytes);
+      const int64_t half = chunk / 2 * width;
+      return both(half, 1, 1, half, 1, 1, bytes - half);
+    }
+    const int64_t total = outer * inner * chunk, n = (total + reorder_tile() - 1) / reorder_tile();
+    const int place = dst == src;
+    if (p.count == kReorderStates || tiles + n > 0x7fffffff || (p.count > 0 && p.place != place)) flush();
+    ReorderState &st = p.st[p.count++];
+    st.src = src;
+    st.dst = dst;
+    st.outer_stride = a.outer_stride;
+    st.row_stride = a.row_stride;
+    st.inner_stride = a.inner_stride;
+    st.total = (uint32_t)total;
+    st.chunk = divisor((uint32_t)chunk);
+    st.per = divisor((uint32_t)(inner * chunk));
+    st.width = (int)width;
+    st.first_tile = (int)tiles;
+    p.place = place;
+    tiles += n;
+  }
+};
+
 }  // namespace
 
 extern "C" {
@@ -113,46 +171,25 @@ archead_status archead_beam_reorder(const archead_beam_state *states, int count,
       return ARCHEAD_ERR_INVALID_ARG;
   }
   const int most = reorder_vector_bytes(beams);
-  ReorderParams p;
-  p.parents = parents;
-  p.batch = batch;
-  p.beams = beams;
-  int i = 0;
-  while (i < count) {
-    // In place and into another buffer are launches of their own.
-    p.count = 0;
-    p.place = states[i].out == nullptr;
-    int64_t tiles = 0;
-    for (; i < count && p.count < kReorderStates && (states[i].out == nullptr) == (p.place != 0); ++i) {
-      const archead_beam_state &a = states[i];
-      const int64_t bytes = a.bytes + length * a.bytes_per_position;
-      if (bytes == 0 || a.outer == 0 || a.inner == 0) continue;
-      char *dst = static_cast<char *>(p.place ? a.data : a.out);
-      const int64_t width = std::min<int64_t>(
-          {(int64_t)most, low_bits((int64_t)(intptr_t)a.data), low_bits((int64_t)(intptr_t)dst), low_bits(bytes),
-           a.outer > 1 ? low_bits(a.outer_stride) : 16, rows > 1 ? low_bits(a.row_stride) : 16,
-           a.inner > 1 ? low_bits(a.inner_stride) : 16});
-      ReorderState &st = p.st[p.count];
-      st.src = static_cast<const char *>(a.data);
-      st.dst = dst;
-      st.outer_stride = a.outer_stride;
-      st.row_stride = a.row_stride;
-      st.inner_stride = a.inner_stride;
-      st.inner = (int)a.inner;
-      st.width = (int)width;
-      st.chunk = bytes / width;
-      st.total = st.chunk * a.inner * a.outer;
-      const int64_t n = (st.total + kReorderTile - 1) / kReorderTile;
-      if (n > 0x7fffffff) return ARCHEAD_ERR_UNSUPPORTED;
-      if (tiles + n > 0x7fffffff) break;  // the next launch
-      st.first_tile = (int)tiles;
-      tiles += n;
-      ++p.count;
-    }
-    p.tiles = (int)tiles;
-    if (p.count > 0) AH_TRY(launch_beam_reorder(p, static_cast<cudaStream_t>(stream)));
+  Reordering r;
+  r.p.parents = parents;
+  r.p.batch = batch;
+  r.p.beams = beams;
+  r.p.count = 0;
+  r.stream = static_cast<cudaStream_t>(stream);
+  for (int i = 0; i < count; ++i) {
+    const archead_beam_state &a = states[i];
+    const int64_t bytes = a.bytes + length * a.bytes_per_position;
+    if (bytes == 0 || a.outer == 0 || a.inner == 0) continue;
+    char *src = static_cast<char *>(a.data), *dst = a.out ? static_cast<char *>(a.out) : src;
+    const int64_t width = std::min<int64_t>(
+        {(int64_t)most, low_bits((int64_t)(intptr_t)src), low_bits((int64_t)(intptr_t)dst), low_bits(bytes),
+         a.outer > 1 ? low_bits(a.outer_stride) : 16, rows > 1 ? low_bits(a.row_stride) : 16,
+         a.inner > 1 ? low_bits(a.inner_stride) : 16});
+    r.add(src, dst, a.outer, a.inner, bytes, a, width);
   }
-  return ARCHEAD_OK;
+  r.flush();
+  return status_of(r.failed);
 }
 
 }  // extern "C"

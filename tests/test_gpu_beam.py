@@ -455,3 +455,22 @@ def test_reorder_on_a_stream_and_in_a_graph():
     on.copy_(parents)
     graph.replay()
     assert torch.equal(dev.cpu(), _reordered(want, parents, ...))
+
+
+@pytest.mark.parametrize("start", [0, 1])
+def test_reorder_more_vectors_than_31_bits(start):
+    """Rows of 2^31 + some single bytes (nothing is aligned): they are moved in parts."""
+    torch = _torch()
+    n, beams = (1 << 31) + 4097, 2
+    buf = torch.empty(beams * n + 16, dtype=torch.uint8, device="cuda")
+    view = buf[start:start + beams * n].view(beams, n)
+    for k in range(beams):
+        view[k] = 0
+        view[k, ::9973] = k + 1
+        view[k, -1] = 100 + k
+    want = [(int((view[k] == k + 1).sum()), 100 + k) for k in range(beams)]
+    parents = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda")
+    archead.archead_beam_reorder(archead.archead_beam_states([archead.archead_beam_state(view)]), parents)
+    for k in range(beams):
+        assert (int((view[k] == 2 - k).sum()), int(view[k, -1])) == want[1 - k]
+        assert bool((view[k, ::9973][:-1] == 2 - k).all())
