@@ -5,9 +5,9 @@
 // all beams of a batch entry: it reads the vectors of the parents and then writes
 // those of the rows that change, so that the exchange needs no second buffer and
 // no order among blocks.  Its place costs two divisions by constants.  Moving two
-// of each four beams of 32 caches of 3001 positions in place (3.1 GB) takes 453 us,
-// the copy rate; with blocks of 256 threads 468, with two vectors a thread 509,
-// with 64-bit divisions 549.  In place, rows that keep their contents are
+// of each four beams of 32 caches of 3001 positions in place (3.1 GB) takes 449 us,
+// the copy rate; with blocks of 256 threads 468, with two vectors a thread 509, with
+// a branch around what lies past the end 490, with 64-bit divisions 549.  In place, rows that keep their contents are
 // neither read (unless another beam takes them) nor written; a parent that
 // several beams take comes from the first-level cache the second time.
 #include <algorithm>
@@ -28,6 +28,7 @@ template <int kMax, typename T>
 __device__ __forceinline__ void move_rows(const ReorderState &st, const int *parent, int beams, bool place, int64_t row0,
                                           uint32_t n, T zero) {
   const uint32_t o = divided(n, st.per), in = n - o * st.per.d, i = divided(in, st.chunk);
+  const bool there = n < st.total;
   const int64_t offset =
       row0 * st.row_stride + o * st.outer_stride + i * st.inner_stride + (int64_t)(in - i * st.chunk.d) * sizeof(T);
   const char *src = st.src + offset;
@@ -36,14 +37,14 @@ __device__ __forceinline__ void move_rows(const ReorderState &st, const int *par
 #pragma unroll
   for (int k = 0; k < kMax; ++k) {
     v[k] = zero;
-    if (k < beams) {
+    if (k < beams && there) {
       const int q = parent[k];
       if (q >= 0 && !(place && q == k)) v[k] = *reinterpret_cast<const T *>(src + q * st.row_stride);
     }
   }
 #pragma unroll
   for (int k = 0; k < kMax; ++k)
-    if (k < beams && !(place && parent[k] == k)) *reinterpret_cast<T *>(dst + k * st.row_stride) = v[k];
+    if (k < beams && there && !(place && parent[k] == k)) *reinterpret_cast<T *>(dst + k * st.row_stride) = v[k];
 }
 
 template <int kMax>
@@ -67,7 +68,6 @@ __global__ void __launch_bounds__(kThreads) beam_reorder_kernel(const __grid_con
       parent[threadIdx.x] = q;
     }
     if (!__syncthreads_or(threadIdx.x < p.beams && !(p.place && q == (int)threadIdx.x))) continue;
-    if (n >= st.total) continue;
     const int64_t row0 = b * p.beams;
     if (kMax <= 16 && st.width == 16)
       move_rows<kMax>(st, parent, p.beams, p.place, row0, n, make_uint4(0, 0, 0, 0));
