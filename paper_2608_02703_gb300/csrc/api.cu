@@ -392,12 +392,16 @@ cudaError_t opt_in_smem(const void *func, int bytes) {
   if (e != cudaSuccess) return e;
   static std::mutex mu;
   static std::map<std::pair<const void *, int>, int> opted;  // (kernel, device) -> bytes
-  std::lock_guard<std::mutex> lock(mu);
-  int &have = opted[{func, dev}];
-  if (have >= bytes) return cudaSuccess;
-  e = cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) have = bytes;
-  return e;
+  try {  // (no exception may leave a C entry)
+    std::lock_guard<std::mutex> lock(mu);
+    int &have = opted[{func, dev}];
+    if (have >= bytes) return cudaSuccess;
+    e = cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) have = bytes;
+    return e;
+  } catch (...) {
+    return cudaErrorMemoryAllocation;
+  }
 }
 
 void timer_begin(archead_pack *p, const char *name, cudaStream_t s, cudaEvent_t *ev0) {
