@@ -664,16 +664,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
 
 }  // namespace
 
-// Blocks of a row: about two a multiprocessor in all, whose starts and ends then
-// overlap, and no fewer than one and a half (128 rows of 151936 in fp32: two
-// 24.4 us, seven 25.6, one 26.0; 160 rows of which 64 have ended, 262144 in bf16:
-// seven 25.7 us, one 34.7); with more rows than multiprocessors take, two a row,
-// so that these come out even (512 rows in bf16 40 us, with one 46).
+// Blocks of a row.  Up to one row a multiprocessor: about two blocks a
+// multiprocessor in all, whose starts and ends then overlap, and no fewer than one
+// and a half (128 rows of 151936 in fp32: two a row 22.0 us, three 23.7, one 23.9;
+// 32 rows in bf16: nine 10.2 us, four 10.9, sixteen 11.3).  More rows: blocks of
+// some 49000 logits, many enough that rows that have ended leave no multiprocessor
+// idle (160 rows of 262144 in bf16, 64 of them ended: five a row 21.4 us, two 26.0,
+// one 32.9, and with none ended 28.6, 27.2, 33.0; 512 rows of 151936: three 33.1 us,
+// two 35.8, six 36.2; 300 rows of 20000 in fp32: one 13.2 us, two 15.0).
+constexpr int kSliceSegments = 96;
 static int beam_slices(int64_t rows, int64_t segments, int sm_count) {
   const int64_t most = (segments + kWarps - 1) / kWarps;
   int64_t n = 2 * sm_count / rows;
   if (2 * rows * n < 3 * sm_count) ++n;
-  if (2 * rows > 3 * sm_count) n = 2;
+  if (rows > sm_count) n = std::max<int64_t>(1, (segments + kSliceSegments / 2) / kSliceSegments);
   return (int)std::min(most, n);
 }
 
@@ -682,7 +686,8 @@ static size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t beam_counter_bytes(int64_t max_rows) { return up((size_t)max_rows * sizeof(int)); }
 size_t beam_scratch_bytes(int64_t max_rows, int64_t max_vocab, int sm_count) {
   const size_t segments = (size_t)((max_vocab + kSegment - 1) / kSegment);
-  return beam_counter_bytes(max_rows) + up((size_t)(2 * max_rows + 4 * sm_count) * sizeof(float2)) +
+  const size_t blocks = (size_t)max_rows * (segments / kSliceSegments + 1) + 4 * sm_count;
+  return beam_counter_bytes(max_rows) + up(blocks * sizeof(float2)) +
          (size_t)max_rows * segments * sizeof(float);
 }
 
