@@ -73,7 +73,7 @@ cudaError_t launch_int8_pad(const int8_t *codes, int64_t M, int K, int K_pad, vo
 cudaError_t launch_int8_decode(const archead_int8_weight *w, const void *x, int dtype, int64_t ldx,
                                const float *x_scales, int64_t M, I8Out out, cudaStream_t s);
 // Most activations that every block quantises for itself (4 tokens of 4096:
-// 7.9 us for 4096 channels, 8.8 with a launch of its own; 8 tokens: 11.4 and 8.8).
+// 6.5 us for 4096 channels, 7.6 with a launch of its own; 8 tokens: 8.7 and 7.4).
 constexpr int64_t kI8FusedQuantize = 16384;
 bool int8_decode_quantizes(int64_t M, int K, int K_pad);
 bool int8_decode_fits(int64_t M, int K_pad);  // all M tokens in one launch

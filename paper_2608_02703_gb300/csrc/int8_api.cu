@@ -27,25 +27,31 @@ size_t take(size_t &off, size_t bytes) {
   return o;
 }
 
-// AUTO takes the warp-level kernel up to 8 tokens, and up to 16 or 32 where the
-// weight is small: each further eight tokens cost its integer MMAs as much
-// again, the tensor-memory kernel costs its start.  Measured, us: 16 tokens of
-// 4096 x 512 3.7 against 5.0, of 4096 x 4096 8.6 against 7.7; 24 tokens of 1000 x
-// 1000 5.6 against 6.0, of 4096 x 1024 6.3 against 6.6.
-bool auto_decodes(const archead_int8_weight *w, int64_t M) {
-  const int64_t size = w->N_pad * w->K_pad;
-  return M <= 8 || (int8_decode_fits(M, w->K_pad) &&
-                    ((M <= 16 && size <= (int64_t)8 << 20) || (M <= 32 && size <= (int64_t)4 << 20)));
-}
-
 // What a call is given: activations, or codes.
 enum Given { kActivations, kCodes };
 
+// Whether the warp-level kernel takes what it is given as it is.
+bool takes_directly(const archead_int8_weight *w, int64_t M, Given given) {
+  return given == kActivations ? int8_decode_quantizes(M, w->K, w->K_pad) : int8_decode_fits(1, w->K_pad);
+}
+
+// AUTO takes the warp-level kernel up to 8 tokens, where its integer sums are
+// exact (the tensor-memory kernel's are up to 2^24; 8 tokens of 16384 x 4096 14.1 us,
+// with that one 12.4, of 4096 x 4096 7.3 and 7.6), and up to 16 where the weight
+// is small: a second eight tokens cost its MMAs as much again, the tensor-memory
+// kernel costs its start.  16 activations of 4096 x 512 4.6 us against 5.6, of
+// 2048 x 2048, which take a launch more, 6.2 against 6.5, of 4096 x 2048 7.5 and
+// 6.6, codes 5.7 and 6.4; 24 tokens of 4096 x 512 6.4 and 5.5.
+bool auto_decodes(const archead_int8_weight *w, int64_t M, Given given) {
+  if (M <= 8) return true;
+  const int64_t most = (int64_t)(takes_directly(w, M, given) ? 8 : 4) << 20;
+  return M <= 16 && int8_decode_fits(M, w->K_pad) && w->N_pad * w->K_pad <= most;
+}
+
 Plan plan(const archead_int8_weight *w, int64_t M, Given given, archead_path path) {
   Plan p;
-  p.gemm = path == ARCHEAD_PATH_PREFILL || (path == ARCHEAD_PATH_AUTO && !auto_decodes(w, M));
-  // The warp-level kernel takes what it is given where it can.
-  p.direct = !p.gemm && (given == kActivations ? int8_decode_quantizes(M, w->K, w->K_pad) : int8_decode_fits(1, w->K_pad));
+  p.gemm = path == ARCHEAD_PATH_PREFILL || (path == ARCHEAD_PATH_AUTO && !auto_decodes(w, M, given));
+  p.direct = !p.gemm && takes_directly(w, M, given);
   if (!p.direct) p.x_off = take(p.total, (size_t)M * w->K_pad * (p.gemm ? 2 : 1));
   if (!p.direct && given == kActivations) p.scale_off = take(p.total, (size_t)M * sizeof(float));
   if (p.gemm) p.g = int8_gemm_plan(w, M);
@@ -56,7 +62,7 @@ Plan plan(const archead_int8_weight *w, int64_t M, Given given, archead_path pat
 // most tokens that the warp-level kernel does not take as they are.
 size_t room_for(const archead_int8_weight *w, int64_t M) {
   size_t most = plan(w, M, kActivations, ARCHEAD_PATH_AUTO).total;
-  for (int64_t m : {8, 16, 32})
+  for (int64_t m : {8, 16})
     if (m < M) most = std::max(most, plan(w, m, kActivations, ARCHEAD_PATH_AUTO).total);
   return most;
 }

@@ -92,6 +92,29 @@ def test_quantize_equals_definition(dtype, M, K, ldx):
     np.testing.assert_array_equal(codes.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("K", [1, 7, 8, 9, 241, 248, 249, 985, 992, 993, 1985, 3968, 7929, 7936, 7951, 9001])
+def test_quantize_rows_on_any_element(dtype, K):
+    """Rows that start on every element of 16 bytes and end on every one: what lies
+    between rows does not count, what lies around the codes is not written."""
+    torch = _torch()
+    g = torch.Generator().manual_seed(K)
+    for offset in range(4 if dtype == "fp32" else 8):
+        M, ldx = 9, K + (0, 1, 3, 4)[(offset + K) % 4]
+        x = torch.randn((M, K), generator=g).to(_dtype(dtype))
+        buf = torch.full((offset + M * ldx + 16,), float("nan") if offset % 2 else 3e4, dtype=_dtype(dtype))
+        rows = buf[offset:offset + M * ldx].view(M, ldx)
+        rows[:, :K] = x
+        on_gpu = buf.cuda()
+        out = torch.full((16 + M * K + 16,), 99, dtype=torch.int8, device="cuda")
+        codes, scales = out[16:16 + M * K].view(M, K), torch.full((M,), -1.0, device="cuda")
+        archead.archead_int8_quantize_tokens(on_gpu[offset:offset + M * ldx].view(M, ldx)[:, :K], codes, scales)
+        want, s = _quantized(x.float().numpy())
+        np.testing.assert_array_equal(scales.cpu().numpy(), s)
+        np.testing.assert_array_equal(codes.cpu().numpy(), want)
+        assert bool((out[:16] == 99).all()) and bool((out[16 + M * K:] == 99).all())
+
+
 def test_quantize_edge_rows():
     """Zero rows, values at half steps (ties to even), the smallest and largest scales, infinities and NaNs."""
     torch = _torch()
