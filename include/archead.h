@@ -409,8 +409,8 @@ ARCHEAD_API archead_status archead_dequant_residual_sc4(const int8_t *codes, con
  *
  * A weight holds its codes in the kernels' layout and serves one stream at a
  * time, like a pack: it owns the scratch of its calls (converted token codes
- * and partial sums), which grows on demand after a device synchronisation (in a
- * stream that is being captured a call that would need more answers
+ * and their scales), which grows on demand after a device synchronisation (in
+ * a stream that is being captured a call that would need more answers
  * ARCHEAD_ERR_UNSUPPORTED).  A call leaves room for every AUTO call with fewer
  * tokens; a new weight has room for 64.
  *

@@ -2,7 +2,9 @@
 // candidates, value = (score - lse) + logit, the n largest (include/archead.h).
 //
 // One launch that reads the logits once and a few of them again; bound by
-// memory, at few rows by latency.  A warp takes segments of 512 logits (16 a
+// memory, at few rows by latency (512 rows of 151936 in fp32 57 us, 80% of the copy
+// rate, 128 rows 22 us, 52%; 4 rows 8.7 us, of which some 3 are the reading and the
+// launch, the rest the merge's steps, each of which waits for the one before).  A warp takes segments of 512 logits (16 a
 // lane, copied some segments ahead into shared memory by asynchronous copies
 // that each thread waits for itself) and keeps, without meeting any other, its
 // lanes' sums of exp(l - m) for a reference m near the maximum; each segment
