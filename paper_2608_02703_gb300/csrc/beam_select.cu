@@ -72,6 +72,16 @@ __device__ __forceinline__ float exp2_of(float d) {
   return y;
 }
 
+// The largest of three; of the warp's.  NaNs are left out unless all are.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  asm("max.f32 %0, %0, %1, %2;\n" : "+f"(a) : "f"(b), "f"(c));
+  return a;
+}
+__device__ __forceinline__ float warp_max(float v) {
+  asm("redux.sync.max.f32 %0, %0, 0xffffffff;\n" : "+f"(v));
+  return v;
+}
+
 // A thread's sum of exp(l - m) for a reference m: a maximum seen before, replaced
 // when a logit passes it by 16 (terms stay below e^16, whose sums fp32 holds as
 // exactly as any).  It is kept as sum of 2^(l log2e - c) with c = m log2e
@@ -175,9 +185,9 @@ struct Raw {
         m = __hmax2(m, reinterpret_cast<const __nv_bfloat162 *>(&r[i / 4])[i % 4]);
       return fmaxf(__low2float(m), __high2float(m));
     } else {
-      float m = x[0];
+      float m = fmaxf(x[0], x[1]);
 #pragma unroll
-      for (int i = 1; i < kE; ++i) m = fmaxf(m, x[i]);
+      for (int i = 2; i < kE; i += 2) m = max3(m, x[i], x[i + 1]);
       return m;
     }
   }
@@ -390,8 +400,8 @@ __device__ void reduce_slice(const SelectParams &p, int r, int sl, uint4 *ring, 
     float x[kE];
     raw.values(x);
     const float top = raw.top(x);
-    const uint32_t most = __reduce_max_sync(0xffffffffu, top >= -INFINITY ? ordered(top) : 0);  // (a NaN: none)
-    if (lane == 0) tops[s] = most ? unordered(most) : -INFINITY;
+    const float most = warp_max(top);
+    if (lane == 0) tops[s] = fmaxf(most, -INFINITY);
     sum.add(x, top);
   }
   asm volatile("cp.async.wait_all;\n" ::: "memory");
@@ -672,8 +682,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 4) beam_select_
 // 32 rows in bf16: nine 10.2 us, four 10.9, sixteen 11.3).  More rows: blocks of
 // some 49000 logits, many enough that rows that have ended leave no multiprocessor
 // idle (160 rows of 262144 in bf16, 64 of them ended: five a row 21.4 us, two 26.0,
-// one 32.9, and with none ended 28.6, 27.2, 33.0; 512 rows of 151936: three 33.1 us,
-// two 35.8, six 36.2; 300 rows of 20000 in fp32: one 13.2 us, two 15.0).
+// one 32.9, and with none ended 28.6, 27.2, 33.0; 512 rows of 151936, 128 of them
+// ended: three 33.1 us, two 35.8, six 36.2; 300 rows of 20000 in fp32, 60 of them
+// ended: one 13.2 us, two 15.0).
 constexpr int kSliceSegments = 96;
 static int beam_slices(int64_t rows, int64_t segments, int sm_count) {
   const int64_t most = (segments + kWarps - 1) / kWarps;
