@@ -85,6 +85,7 @@ struct I8DecodeParams {
   bool vec;        // x: 16-byte loads
   int *err;
   int64_t wait_budget;
+  int64_t drain_budget;  // of the waits for what is in flight when a block ends: no less than the default
 };
 
 // This block's round r.
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_decode_kernel(const I8Decode
       const uint8_t *src = p.codes + tile * p.KC * kSlot + (s & 7) * kSegment;
       for (int e = 0; e < now.steps; ++e) {
         if (!mbar_wait_warp(&empty[slot], ph ^ 1, p.wait_budget, &abort_flag, p.err)) {
-          drain_ring(full, p.slots, issued, p.wait_budget, p.err);
+          drain_ring(full, p.slots, issued, p.drain_budget, p.err);
           return;
         }
         if (leader) {
@@ -327,6 +328,7 @@ cudaError_t launch_int8_decode(const archead_int8_weight *w, const void *x, int 
   p.ldx = ldx;
   p.err = w->err;
   p.wait_budget = w->wait_budget;
+  p.drain_budget = std::max(w->wait_budget, kDefaultWaitBudget);
   // Rounds of kw[0] K stages a slot while every block has one, then rounds of kw[1]
   // >= kw[0] for the strips that are left: the fewest slots for the busiest block,
   // where a round's end costs about as much as two.  (8 tokens of 20000 x 1024 8.0

@@ -84,6 +84,7 @@ struct I8GemmParams {
   int ks_log2;   // log2 of the blocks that share a unit's K
   int *err;
   int64_t wait_budget;
+  int64_t drain_budget;  // of the waits for what is in flight when a block ends: no less than the default
 };
 
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n) {
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
         const int m0 = u % p.num_mt * p.nt;
         for (int e = begin; e < end; ++e) {
           if (!mbar_wait_warp(&x_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
-            drain_copies(x_full, kXS, issued, p.wait_budget, p.err);
+            drain_copies(x_full, kXS, issued, p.drain_budget, p.err);
             goto done;
           }
           if (leader) {
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
         const uint8_t *src = p.codes + (int64_t)(u / p.num_mt) * p.KC * G::kCodeSlot;
         for (int e = begin; e < end; ++e) {
           if (!mbar_wait_warp(&c_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
-            drain_copies(c_full, kCS, issued, p.wait_budget, p.err);
+            drain_copies(c_full, kCS, issued, p.drain_budget, p.err);
             goto done;
           }
           if (leader) {
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
 done:
   if (mma_leader) {
     tc_commit(drain);  // (each issuing thread's)
-    mbar_wait(drain, 0, p.wait_budget, nullptr, p.err);
+    mbar_wait(drain, 0, p.drain_budget, nullptr, p.err);
   }
   if (kSplit && !at_barrier) {  // every thread meets its cluster once, whatever became of its work
     __syncwarp();
@@ -567,6 +568,7 @@ cudaError_t launch_int8_gemm(const archead_int8_weight *w, const I8GemmPlan &f, 
   p.ks_log2 = f.ks_log2;
   p.err = w->err;
   p.wait_budget = w->wait_budget;
+  p.drain_budget = std::max(w->wait_budget, kDefaultWaitBudget);
   if (f.ks_log2 > 0) {
     const int grid = (int)f.units << f.ks_log2;
     return f.NT == 64 ? launch_gemm_t<64, true>(p, grid, s) : launch_gemm_t<128, true>(p, grid, s);

@@ -196,6 +196,24 @@ def test_product_split_and_whole(M, N, K, path):
     w.close()
 
 
+@pytest.mark.parametrize("M", [1, 3, 8, 9, 16])
+@pytest.mark.parametrize("N,K", [(9760, 2001), (10007, 1303), (19473, 200), (20000, 1024), (39000, 640)], ids=str)
+def test_few_tokens_in_rounds_of_two_kinds(M, N, K):
+    """Channels that all multiprocessors take in whole rounds, and a rest that is cut along K."""
+    torch = _torch()
+    a = _draw(M, N, K, seed=N + M)
+    w = archead.archead_int8_weight_create(a[0], a[1])
+    y = torch.full((M, N), float("nan"), dtype=torch.float32, device="cuda")
+    archead.archead_int8_matmul_path(w, _dev(a[2]), _dev(a[3]), M, y, archead.PATH_DECODE)
+    _check(y, _want(*a), "fp32")
+    x = torch.randn((M, K), generator=torch.Generator().manual_seed(M)).to(torch.bfloat16)
+    q, s = _quantized(x.float().numpy())
+    archead.archead_int8_linear(w, x.cuda(), M, y)
+    _check(y, _want(a[0], a[1], q, s), "fp32")
+    assert archead.archead_int8_sync_status(w) == archead.OK
+    w.close()
+
+
 @pytest.mark.parametrize("M", [1, 8, 20, 40, 64, 100, 128, 200, 300])
 def test_wide_weights_from_memory(M):
     """Many units a block, whose codes come from memory (more of them than the second-level cache holds) and so in any
