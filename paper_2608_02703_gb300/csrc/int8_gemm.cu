@@ -20,9 +20,9 @@
 //     eight MMAs, which run 312 for 64 tokens and 536 for 128);
 //   - epilogue warps read the accumulators, scale, round and store.
 //
-// Bound: by the tensor cores from some 128 tokens on (2048 tokens of 151936 x 4096
-// 1.40 ms, 97% of the rate that the library's bf16 product reaches), by memory for
-// fewer of a large weight (64 tokens 101 us, 94% of the copy rate), and by its
+// Bound: by the tensor cores from some 200 tokens on (512 tokens of 151936 x 4096
+// 343 us, 2048 1.38 ms: 98% of the rate that the library's bf16 product reaches), by
+// memory for fewer of a large weight (64 tokens 100 us, 128 105: 93%), and by its
 // start, its stages' pace and its join for a small weight (64 tokens of 4096 x 512
 // 5.7 us, the quantiser's launch included).
 #include <cuda_fp16.h>
@@ -183,6 +183,16 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
   const int ks = kSplit ? 1 << p.ks_log2 : 1, slice = kSplit ? (int)blockIdx.x & (ks - 1) : 0;
   const int u0 = kSplit ? (int)blockIdx.x >> p.ks_log2 : (int)blockIdx.x, step = kSplit ? p.units : (int)gridDim.x;
   const int begin = kSplit ? p.KC * slice / ks : 0, end = kSplit ? p.KC * (slice + 1) / ks : p.KC;
+  // Over several rounds half of the tiles at work start in the middle of K: all read
+  // the same tokens, and did so at the same time from the same places of L2 (128
+  // tokens of 151936 x 4096 115 us, with this 105; 256 210 and 179, 512 383 and 338; with
+  // four starts or eight 345 and 350).  In one round there is nothing to gain (512
+  // tokens of 4096 x 4096 16.6 us and 16.8).
+  const int at_once = p.units <= (int)gridDim.x ? 0 : max(2, (int)gridDim.x / p.num_mt);
+  const auto first_of = [&](int u) {
+    if constexpr (kSplit) return begin;
+    return at_once > 0 && 2 * (u / p.num_mt % at_once) >= at_once ? (begin + end) / 2 : begin;
+  };
   bool at_barrier = false;  // this thread has met the cluster
 
   if (warp < 4) {
@@ -195,7 +205,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       asm volatile("griddepcontrol.wait;\n" ::: "memory");  // the widened codes come from the grid before
       for (int u = u0; u < p.units; u += step) {
         const int m0 = u % p.num_mt * p.nt;
-        for (int e = begin; e < end; ++e) {
+        for (int e = begin, k = first_of(u); e < end; ++e, k = k + 1 < end ? k + 1 : begin) {
           if (!mbar_wait_warp(&x_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
             drain_copies(x_full, kXS, issued, p.drain_budget, p.err);
             goto done;
@@ -203,8 +213,8 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
           if (leader) {
             uint8_t *dst = smem + r.s * G::kXBytes;
             mbar_arrive_expect_tx(&x_full[r.s], (uint32_t)p.nt * 256);
-            tma_load_2d(dst, &p.tmap_x, e * 128, m0, &x_full[r.s]);
-            tma_load_2d(dst + G::kBoxBytes, &p.tmap_x, e * 128 + 64, m0, &x_full[r.s]);
+            tma_load_2d(dst, &p.tmap_x, k * 128, m0, &x_full[r.s]);
+            tma_load_2d(dst + G::kBoxBytes, &p.tmap_x, k * 128 + 64, m0, &x_full[r.s]);
           }
           ++issued;
           r.next();
@@ -218,14 +228,14 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       int issued = 0;
       for (int u = u0; u < p.units; u += step) {
         const uint8_t *src = p.codes + (int64_t)(u / p.num_mt) * p.KC * G::kCodeSlot;
-        for (int e = begin; e < end; ++e) {
+        for (int e = begin, k = first_of(u); e < end; ++e, k = k + 1 < end ? k + 1 : begin) {
           if (!mbar_wait_warp(&c_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
             drain_copies(c_full, kCS, issued, p.drain_budget, p.err);
             goto done;
           }
           if (leader) {
             mbar_arrive_expect_tx(&c_full[r.s], G::kCodeSlot);
-            bulk_g2s(smem + G::kCodeOff + r.s * G::kCodeSlot, src + (int64_t)e * G::kCodeSlot, G::kCodeSlot,
+            bulk_g2s(smem + G::kCodeOff + r.s * G::kCodeSlot, src + (int64_t)k * G::kCodeSlot, G::kCodeSlot,
                      &c_full[r.s]);
           }
           ++issued;
