@@ -21,7 +21,7 @@
 //   - epilogue warps read the accumulators, scale, round and store.
 //
 // Bound: by the tensor cores from some 200 tokens on (512 tokens of 151936 x 4096
-// 343 us, 2048 1.38 ms: 98% of the rate that the library's bf16 product reaches), by
+// 343 us, 2048 1.42 ms: 96% of the rate that the library's bf16 product reaches), by
 // memory for fewer of a large weight (64 tokens 100 us, 128 105: 93%), and by its
 // start, its stages' pace and its join for a small weight (64 tokens of 4096 x 512
 // 5.7 us, the quantiser's launch included).
