@@ -380,6 +380,8 @@ def _rows(t, rows: int, cols: int, what: str) -> int:
     if len(shape) != 2 or shape[0] < rows or shape[1] != cols or (stride[1] != 1 and cols > 1):
         raise ValueError(f"{what}: {rows} rows of {cols} adjacent elements are wanted, "
                          f"not {tuple(shape)} with strides {stride}")
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on the GPU")
     return stride[0] if shape[0] > 1 else cols
 
 
@@ -387,6 +389,8 @@ def _flat(t, dtype, size: int, what: str):
     """Address of a contiguous tensor of at least `size` elements of the type."""
     if t.dtype is not dtype or t.numel() < size or not t.is_contiguous():
         raise ValueError(f"{what}: {size} contiguous elements of {dtype} are wanted, not {tuple(t.shape)} of {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on the GPU")
     return t.data_ptr()
 
 
@@ -600,6 +604,7 @@ class BeamStates:
         self.rows = min((s.rows for s in states), default=0)
         self.room = min((s.room for s in states if s.room is not None), default=None)
         self.tensors = [s.tensors for s in states]  # (their memory is kept)
+        self.on_gpu = all(t.is_cuda for pair in self.tensors for t in pair if t is not None)
 
 
 def archead_beam_states(states: List[BeamState]) -> BeamStates:
@@ -615,6 +620,8 @@ def archead_beam_reorder(states: BeamStates, parents, length: int = 0, stream=No
     if states.count and (batch * beams > states.rows or (states.room is not None and length > states.room)):
         raise ValueError(f"{batch * beams} rows of {length} positions in states of {states.rows} rows and "
                          f"{states.room} positions")
+    if not states.on_gpu:
+        raise ValueError("a state is not on the GPU")
     _check(load().archead_beam_reorder(states.array, states.count, _flat(parents, torch.int32, batch * beams, "parents"),
                                        batch, beams, length, _stream_at(stream, parents)), "archead_beam_reorder")
 

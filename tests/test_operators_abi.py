@@ -184,3 +184,19 @@ def test_binding_refuses_shapes_and_types():
         with pytest.raises(ValueError):
             archead.archead_beam_select(beam, **(good | kw))
     assert f32 == y.dtype
+
+
+def test_binding_refuses_tensors_on_the_host():
+    import torch
+
+    w, beam = archead.Int8Weight(None, 10, 6), archead.Beam(None)
+    x, y, c, s = torch.empty((3, 6)), torch.empty((3, 10)), torch.empty((3, 6), dtype=torch.int8), torch.empty(3)
+    i = torch.zeros((2, 4), dtype=torch.int32)
+    states = archead.archead_beam_states([archead.archead_beam_state(torch.empty((8, 5)))])
+    for bad in (lambda: archead.archead_int8_linear(w, x, 3, y), lambda: archead.archead_int8_matmul(w, c, s, 3, y),
+                lambda: archead.archead_int8_quantize_tokens(x, c, s),
+                lambda: archead.archead_beam_select(beam, torch.empty((8, 9)), torch.empty((2, 4)), torch.empty((2, 4)),
+                                                    i, i),
+                lambda: archead.archead_beam_reorder(states, i)):
+        with pytest.raises(ValueError, match="GPU"):
+            bad()
