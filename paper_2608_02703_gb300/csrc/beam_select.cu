@@ -2,13 +2,15 @@
 // candidates, value = (score - lse) + logit, the n largest (include/archead.h).
 //
 // One launch that reads the logits once and a few of them again; bound by
-// memory, at few rows by latency (512 rows of 151936 in fp32 57 us, 80% of the copy
-// rate, 128 rows 22 us, 52%; 4 rows 8.7 us, of which some 3 are the reading and the
-// launch, the rest the merge's steps, each of which waits for the one before).  A warp takes segments of 512 logits (16 a
-// lane, copied some segments ahead into shared memory by asynchronous copies
-// that each thread waits for itself) and keeps, without meeting any other, its
-// lanes' sums of exp(l - m) for a reference m near the maximum; each segment
-// leaves its largest logit.  The block that finishes last of a batch entry
+// memory, at few rows by latency (512 rows of 151936 in fp32 57 us, 81% of the copy
+// rate, 128 rows 21 us, 54%; 4 rows 8.2 us, of which some 3 are the reading and the
+// launch, the rest the merge's steps, each of which waits for the one before).
+//
+// A warp takes segments of 512 logits (16 a lane, copied some segments ahead into
+// shared memory by asynchronous copies that each thread waits for itself) and
+// keeps, without meeting any other, its lanes' sums of exp(l - m) for a reference
+// m near the maximum; each segment leaves its largest logit.  The block that
+// finishes last of a batch entry
 //   - joins the blocks' sums, in their order, into each beam's log-sum-exp;
 //   - finds the n best segments by their largest values: no other holds one of
 //     the n best candidates;
