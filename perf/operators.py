@@ -211,7 +211,8 @@ def prepare(case, seed):
 
 def _plain_quantize(x):
     x = x.float()
-    scales = x.abs().amax(dim=1) / 127
+    top = x.abs().amax(dim=1)
+    scales = top / torch.full_like(top, 127)  # (by a Python number: a product with its rounded reciprocal on the GPU)
     usable = (scales > 0) & torch.isfinite(scales)
     q = torch.round(x / torch.where(usable, scales, 1)[:, None]).clamp(-127, 127)
     return torch.where(usable[:, None], q, 0).to(torch.int8), scales
