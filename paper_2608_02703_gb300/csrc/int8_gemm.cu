@@ -139,6 +139,7 @@ __device__ __forceinline__ void store_channel(const I8Out &o, int64_t m0, int64_
     store_channel<__nv_bfloat16>(o, m0, n, there, acc, cols, xs, sw);
 }
 
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory"); }
 
@@ -174,6 +175,10 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // A block's shared memory may be written by its peers from when it is known to
+  // run: the cluster meets twice, here (waited for by the epilogue before its
+  // first remote store, by the others at the end) and at the join.
+  if constexpr (kSplit) cluster_arrive_relaxed();
   const uint32_t tmem_base = *tmem_slot;
   const uint32_t a_base = tmem_base + kAcc * G::kIssue * NT;
   bool mma_leader = false;
@@ -193,7 +198,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     if constexpr (kSplit) return begin;
     return at_once > 0 && 2 * (u / p.num_mt % at_once) >= at_once ? (begin + end) / 2 : begin;
   };
-  bool at_barrier = false;  // this thread has met the cluster
+  int met = 0;  // times this thread has met its cluster
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegs0) : "memory");
@@ -367,6 +372,10 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     const uint32_t lane_addr = tmem_base + ((uint32_t)(lg * 32) << 16) + col0;
     RingPos<kAcc> accr;
     int stages = 0;  // of the units before, modulo 2
+    if constexpr (kSplit) {
+      cluster_wait();
+      met = 1;
+    }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");  // (the tokens' scales)
     for (int u = u0; u < p.units; u += step) {
       const int64_t n = (int64_t)(u / p.num_mt) * kI8PadN + lg * 32 + lane;
@@ -433,7 +442,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
             xq[c] = 32 * c + lane < min(lim, kMine) ? p.x_scales[mb + 32 * c + lane] : 0.f;
           cluster_arrive();
           cluster_wait();
-          at_barrier = true;
+          met = 2;
           const float *sums = reinterpret_cast<const float *>(smem + G::kJoinOff) + pw * kMine * kI8PadN + lg * 32 + lane;
 #pragma unroll
           for (int i = 0; i < kMine; ++i) v[i] = sums[i * kI8PadN];
@@ -456,8 +465,9 @@ done:
     tc_commit(drain);  // (each issuing thread's)
     mbar_wait(drain, 0, p.drain_budget, nullptr, p.err);
   }
-  if (kSplit && !at_barrier) {  // every thread meets its cluster once, whatever became of its work
+  if (kSplit && met < 2) {  // every thread meets its cluster twice, whatever became of its work
     __syncwarp();
+    if (met == 0) cluster_wait();
     cluster_arrive();
     cluster_wait();
   }

@@ -1,0 +1,44 @@
+"""The protocols of the INT8 product's kernels: blocks that share K through one another's shared memory."""
+
+import pytest
+
+from paper_2608_02703_gb300 import archead
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _build():
+    from paper_2608_02703_gb300.build import build
+
+    build()
+
+
+def _operands(M, N, K, seed=0):
+    """Codes on the device whose sums stay below 2^24, and the sums."""
+    import torch
+
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    x = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    want = x.double() @ codes.double().t()
+    assert float(want.abs().max()) < 2 ** 24
+    return codes, x, want
+
+
+@pytest.mark.parametrize("M", [17, 40, 64, 65, 100, 128])
+@pytest.mark.parametrize("N,K", [(100, 1024), (128, 512), (1000, 1000), (2400, 1024), (4000, 512), (300, 1100)], ids=str)
+def test_blocks_of_a_stage_or_two_join(M, N, K):
+    """K cut into parts of one or two stages: a block sends its sums as soon as it can after its start."""
+    import torch
+
+    codes, x, want = _operands(M, N, K, seed=M)
+    w = archead.archead_int8_weight_create(codes, torch.ones(N, device="cuda"))
+    ones = torch.ones(M, device="cuda")
+    ys = [torch.full((M, N), float("nan"), device="cuda") for _ in range(20)]
+    for y in ys:  # (back to back)
+        archead.archead_int8_matmul_path(w, x, ones, M, y, archead.PATH_PREFILL)
+    assert archead.archead_int8_sync_status(w) == archead.OK
+    for y in ys:
+        assert torch.equal(y.double(), want)
+    w.close()
