@@ -110,7 +110,8 @@ enum I8Source {
 
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 512;\n" ::: "memory"); }
 
-// After a failed wait: lets the bulk copies issued so far land before the warp ends.
+// Lets the bulk copies issued so far land before the producer ends: a consumer whose
+// wait gives up may let the block end before they have.
 __device__ __forceinline__ void drain_ring(uint64_t *full, int slots, int issued, int64_t budget, int *err) {
   for (int k = issued > slots ? issued - slots : 0; k < issued; ++k)
     mbar_wait_warp(&full[k % slots], (uint32_t)(k / slots) & 1, budget, nullptr, err);
@@ -145,10 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_decode_kernel(const I8Decode
       const int64_t s = now.strip, tile = s >> 3;
       const uint8_t *src = p.codes + tile * p.KC * kSlot + (s & 7) * kSegment;
       for (int e = 0; e < now.steps; ++e) {
-        if (!mbar_wait_warp(&empty[slot], ph ^ 1, p.wait_budget, &abort_flag, p.err)) {
-          drain_ring(full, p.slots, issued, p.drain_budget, p.err);
-          return;
-        }
+        if (!mbar_wait_warp(&empty[slot], ph ^ 1, p.wait_budget, &abort_flag, p.err)) goto issued_all;
         if (leader) {
           const int n = tile < p.tiles ? min(kw, p.KC - e * kw) : 0;  // stages there are
           mbar_arrive_expect_tx(&full[slot], (uint32_t)(n * strips * kSegment));
@@ -161,6 +159,8 @@ __global__ void __launch_bounds__(kThreads, 1) int8_decode_kernel(const I8Decode
         if (++slot == p.slots) slot = 0, ph ^= 1;
       }
     }
+  issued_all:
+    drain_ring(full, p.slots, issued, p.drain_budget, p.err);
     return;
   }
 
@@ -231,7 +231,9 @@ __global__ void __launch_bounds__(kThreads, 1) int8_decode_kernel(const I8Decode
     int d[kTiles][4] = {};
     for (int e = 0; e < now.steps; ++e, turn ^= 1) {
       if (turn != half) continue;
-      // After a wait that gave up the loops go on without work, for the barriers below.
+      // After a wait that gave up the loops go on for the barriers below, without
+      // work and without releasing a slot that this warp has not seen full: the
+      // producer would copy into one whose copy is under way.
       ok = ok && mbar_wait_warp(&full[slot], ph, p.wait_budget, &abort_flag, p.err);
       const int kc = e * kw + q;
       if (ok && kc < p.KC) {
@@ -250,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) int8_decode_kernel(const I8Decode
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[slot]);
+      if (ok && lane == 0) mbar_arrive(&empty[slot]);
       slot += 2;
       if (slot >= p.slots) slot = half, ph ^= 1;
     }

@@ -1,4 +1,5 @@
-"""The protocols of the INT8 product's kernels: blocks that share K through one another's shared memory."""
+"""The protocols of the INT8 product's kernels: blocks that share K through one another's shared memory,
+and waits that give up."""
 
 import pytest
 
@@ -41,4 +42,42 @@ def test_blocks_of_a_stage_or_two_join(M, N, K):
     assert archead.archead_int8_sync_status(w) == archead.OK
     for y in ys:
         assert torch.equal(y.double(), want)
+    w.close()
+
+
+@pytest.fixture(scope="module")
+def long_row():
+    """Work of some milliseconds in one block: the quantisation of a single long row.  It lets the kernel behind it
+    start at once, whose warps that need what it computes then wait for its end, and others for those."""
+    import torch
+
+    x = torch.zeros((1, 1 << 28), dtype=torch.bfloat16, device="cuda")
+    codes, scales = torch.empty(x.shape, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+    return lambda: archead.archead_int8_quantize_tokens(x, codes, scales)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 40000, 4096), (8, 30000, 2048), (16, 20000, 2501), (3, 20000, 9000)], ids=str)
+def test_few_tokens_a_wait_that_gives_up(M, N, K, long_row):
+    """The copying warp waits for slots that nobody frees meanwhile (a block has more stages than the twelve slots of
+    the largest ring): with a limit of a few cycles it gives up, the call ends, the status says so, and the weight is
+    as good as before once the limit is back."""
+    import torch
+
+    codes, x, want = _operands(M, N, K, seed=M)
+    w = archead.archead_int8_weight_create(codes, torch.ones(N, device="cuda"))
+    ones, y = torch.ones(M, device="cuda"), torch.empty((M, N), device="cuda")
+
+    def call():
+        y.fill_(float("nan"))
+        long_row()
+        archead.archead_int8_matmul_path(w, x, ones, M, y, archead.PATH_DECODE)
+        return archead.archead_int8_sync_status(w)
+
+    assert call() == archead.OK and torch.equal(y.double(), want)
+    for budget in (1, 1000, 100000):
+        archead.archead_int8_set_wait_budget(w, budget)
+        for _ in range(3):
+            assert call() == archead.ERR_DEVICE_TIMEOUT
+        archead.archead_int8_set_wait_budget(w, 2_000_000_000)
+        assert call() == archead.OK and torch.equal(y.double(), want)
     w.close()
