@@ -27,6 +27,8 @@
 // 5.7 us, the quantiser's launch included).
 #include <cuda_fp16.h>
 
+#include <limits.h>
+
 #include <algorithm>
 
 #include "int8_quant.cuh"
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
   uint64_t *drain = acc_empty + kAcc;
   if (G::kOne) x_full = a_full, x_empty = a_empty;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
-  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1), *x_issued = abort_flag + 1;
   const int warp = threadIdx.x >> 5, lane = lane_id();
 
   if (smem_u32(smem) & 1023) {  // the same for every block: nothing has been started
@@ -199,6 +201,8 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
     return at_once > 0 && 2 * (u / p.num_mt % at_once) >= at_once ? (begin + end) / 2 : begin;
   };
   int met = 0;  // times this thread has met its cluster
+  int issued = 0;  // stages whose copies this warp has issued
+  int stopped = INT_MAX;  // stage at which this converter's wait gave up, counted over all units
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegs0) : "memory");
@@ -206,15 +210,11 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       // ------------------------------ tokens ------------------------------
       const bool leader = elect_one();
       RingPos<kXS> r;
-      int issued = 0;
       asm volatile("griddepcontrol.wait;\n" ::: "memory");  // the widened codes come from the grid before
       for (int u = u0; u < p.units; u += step) {
         const int m0 = u % p.num_mt * p.nt;
         for (int e = begin, k = first_of(u); e < end; ++e, k = k + 1 < end ? k + 1 : begin) {
-          if (!mbar_wait_warp(&x_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
-            drain_copies(x_full, kXS, issued, p.drain_budget, p.err);
-            goto done;
-          }
+          if (!mbar_wait_warp(&x_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
           if (leader) {
             uint8_t *dst = smem + r.s * G::kXBytes;
             mbar_arrive_expect_tx(&x_full[r.s], (uint32_t)p.nt * 256);
@@ -230,14 +230,10 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
       // ------------------------------ weight codes ------------------------------
       const bool leader = elect_one();
       RingPos<kCS> r;
-      int issued = 0;
       for (int u = u0; u < p.units; u += step) {
         const uint8_t *src = p.codes + (int64_t)(u / p.num_mt) * p.KC * G::kCodeSlot;
         for (int e = begin, k = first_of(u); e < end; ++e, k = k + 1 < end ? k + 1 : begin) {
-          if (!mbar_wait_warp(&c_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
-            drain_copies(c_full, kCS, issued, p.drain_budget, p.err);
-            goto done;
-          }
+          if (!mbar_wait_warp(&c_empty[r.s], r.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
           if (leader) {
             mbar_arrive_expect_tx(&c_full[r.s], G::kCodeSlot);
             bulk_g2s(smem + G::kCodeOff + r.s * G::kCodeSlot, src + (int64_t)k * G::kCodeSlot, G::kCodeSlot,
@@ -329,8 +325,11 @@ __global__ void __launch_bounds__(I8Geom<NT, kSplit>::kThreads, 1)
         // threads those of stages an even number apart do: kConv, kA and kCS are
         // even then.  (With five code slots a converter could pass a barrier whose
         // copy, from DRAM out of order, had not come.)
-        if (!mbar_wait_warp(&a_empty[ar.s], ar.ph ^ 1, p.wait_budget, abort_flag, p.err)) goto done;
-        if (!mbar_wait_warp(&c_full[cr.s], cr.ph, p.wait_budget, abort_flag, p.err)) goto done;
+        if (!mbar_wait_warp(&a_empty[ar.s], ar.ph ^ 1, p.wait_budget, abort_flag, p.err) ||
+            !mbar_wait_warp(&c_full[cr.s], cr.ph, p.wait_budget, abort_flag, p.err)) {
+          stopped = (u - u0) / step * len + n;
+          goto done;
+        }
         tc_fence_after();
         const uint4 *codes = reinterpret_cast<const uint4 *>(smem + G::kCodeOff + cr.s * G::kCodeSlot) + cw * 256 + lane;
         const uint32_t acol = a_base + ((uint32_t)(cw * 32) << 16) + ar.s * 64;
@@ -465,6 +464,7 @@ done:
     tc_commit(drain);  // (each issuing thread's)
     mbar_wait(drain, 0, p.drain_budget, nullptr, p.err);
   }
+  if (threadIdx.x == 0) *x_issued = issued;
   if (kSplit && met < 2) {  // every thread meets its cluster twice, whatever became of its work
     __syncwarp();
     if (met == 0) cluster_wait();
@@ -476,6 +476,16 @@ done:
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, kPfTmemCols);
+  }
+  // Without a wait that gave up every copy has been used.  Otherwise what is under
+  // way lands before the block ends.  A barrier that a stage's tokens share with its
+  // converters takes first what these owe: nobody else arrives any more, and a stage
+  // is issued only when the one before in its place has been multiplied.
+  if (*abort_flag) {
+    if (warp == 0) drain_copies(x_full, kXS, issued, p.drain_budget, p.err);
+    if (warp == 2) drain_copies(c_full, kCS, issued, p.drain_budget, p.err);
+    if (G::kOne && lane == 0)
+      for (int k = stopped; k < *x_issued; k += G::kConv) mbar_arrive(&a_full[k % kA]);
   }
 }
 

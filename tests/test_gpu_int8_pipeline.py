@@ -81,3 +81,45 @@ def test_few_tokens_a_wait_that_gives_up(M, N, K, long_row):
         archead.archead_int8_set_wait_budget(w, 2_000_000_000)
         assert call() == archead.OK and torch.equal(y.double(), want)
     w.close()
+
+
+@pytest.mark.parametrize("M,N,K", [(17, 128, 131071), (64, 9728, 131071), (64, 19456, 131071), (128, 1000, 131071),
+                                   (128, 19456, 131071), (256, 19456, 131071)], ids=str)
+def test_many_tokens_a_wait_that_gives_up(M, N, K):
+    """The epilogue waits for a unit's whole K: with a limit of a few cycles it gives up while copies, conversions
+    and products are under way.  The call ends without waiting for what nobody completes any more (a limit of a
+    second each), the status says so, and the weight is as good as before once the limit is back."""
+    import time
+
+    import torch
+
+    g = torch.Generator(device="cuda").manual_seed(M)
+    codes = torch.randint(-8, 9, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    x = torch.randint(-8, 9, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    w = archead.archead_int8_weight_create(codes, torch.ones(N, device="cuda"))
+    rows = torch.arange(0, N, max(1, N // 500), device="cuda")
+    want = x.double() @ codes[rows].double().t()  # (exact below 2^24)
+    assert float(want.abs().max()) < 2 ** 24
+    del codes
+    ones, y = torch.ones(M, device="cuda"), torch.empty((M, N), device="cuda")
+
+    def call():
+        y.fill_(float("nan"))
+        torch.cuda.synchronize()
+        t = time.perf_counter()
+        archead.archead_int8_matmul_path(w, x, ones, M, y, archead.PATH_PREFILL)
+        status = archead.archead_int8_sync_status(w)
+        return status, time.perf_counter() - t
+
+    def is_right():
+        return call()[0] == archead.OK and torch.equal(y[:, rows].double(), want)
+
+    assert is_right()
+    for budget in (1, 1000):
+        archead.archead_int8_set_wait_budget(w, budget)
+        for _ in range(3):
+            status, seconds = call()
+            assert status == archead.ERR_DEVICE_TIMEOUT and seconds < 0.3
+        archead.archead_int8_set_wait_budget(w, 2_000_000_000)
+        assert is_right()
+    w.close()
