@@ -412,7 +412,9 @@ ARCHEAD_API archead_status archead_dequant_residual_sc4(const int8_t *codes, con
  * and their scales), which grows on demand after a device synchronisation (in
  * a stream that is being captured a call that would need more answers
  * ARCHEAD_ERR_UNSUPPORTED).  A call leaves room for every AUTO call with fewer
- * tokens; a new weight has room for 64.
+ * tokens; a new weight has room for 64.  Scratch that a captured call was given
+ * stays the weight's when it grows, so that the graph can be replayed as long as
+ * the weight lives.
  *
  * archead_int8_weight_create: codes int8 [N][K] and scales fp32 [N] (host or
  *   device memory, any alignment, read during the call only; the call waits

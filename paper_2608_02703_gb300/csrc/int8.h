@@ -38,6 +38,11 @@ struct archead_int8_weight {
   int clusters[2][4] = {};  // of 2^i blocks of the split tensor-memory kernels (64, 128 tokens) that run at once
   void *ws = nullptr;
   size_t ws_bytes = 0;
+  bool ws_captured = false;  // a captured call holds addresses of ws: it is kept until the weight goes
+  struct Kept {
+    void *ws;
+    Kept *next;
+  } *kept = nullptr;
   int64_t reserved_tokens = 0;  // every AUTO call of up to so many fits
   int64_t owned_bytes = 0;
   int64_t wait_budget = 0;

@@ -68,16 +68,24 @@ size_t room_for(const archead_int8_weight *w, int64_t M) {
 }
 
 // Growing synchronises the device: a call made earlier on another stream may
-// still use the old buffer.
+// still use the old buffer.  One that a captured call was given stays: its graph
+// may run again.  The next is then at least twice as large, so that what is kept is
+// never more than what is in use.
 cudaError_t grow_workspace(archead_int8_weight *w, size_t bytes) {
   cudaError_t e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return e;
-  if (w->ws) {
+  if (w->ws && w->ws_captured) {
+    archead_int8_weight::Kept *k = new (std::nothrow) archead_int8_weight::Kept{w->ws, w->kept};
+    if (!k) return cudaErrorMemoryAllocation;
+    w->kept = k;
+    bytes = std::max(bytes, 2 * w->ws_bytes);
+  } else if (w->ws) {
     cudaFree(w->ws);
     w->owned_bytes -= (int64_t)w->ws_bytes;
-    w->ws = nullptr;
-    w->ws_bytes = 0;
   }
+  w->ws = nullptr;
+  w->ws_bytes = 0;
+  w->ws_captured = false;
   e = cudaMalloc(&w->ws, bytes);
   if (e != cudaSuccess) return e;
   w->ws_bytes = bytes;
@@ -87,13 +95,15 @@ cudaError_t grow_workspace(archead_int8_weight *w, size_t bytes) {
 
 // Room for a call that needs `bytes`, and for every AUTO call of fewer tokens.
 archead_status ensure_workspace(archead_int8_weight *w, size_t bytes, int64_t M, cudaStream_t s) {
+  const bool captured = is_capturing(s);
+  if (captured && bytes <= w->ws_bytes) w->ws_captured = true;
   if (bytes <= w->ws_bytes && M <= w->reserved_tokens) return ARCHEAD_OK;
-  if (M > w->reserved_tokens && !is_capturing(s)) {
+  if (M > w->reserved_tokens && !captured) {
     bytes = std::max(bytes, room_for(w, M));
     w->reserved_tokens = M;
   }
   if (bytes <= w->ws_bytes) return ARCHEAD_OK;
-  if (is_capturing(s)) {
+  if (captured) {
     set_last_error_message("the workspace cannot grow while the stream is captured: call once with as many tokens before");
     return ARCHEAD_ERR_UNSUPPORTED;
   }
@@ -116,6 +126,12 @@ archead_status run_product(archead_int8_weight *w, const Plan &p, const float *x
 void free_weight(archead_int8_weight *w) {
   for (void *b : {(void *)w->codes, (void *)w->scales, (void *)w->err, w->ws})
     if (b) cudaFree(b);
+  while (w->kept) {
+    archead_int8_weight::Kept *k = w->kept;
+    w->kept = k->next;
+    cudaFree(k->ws);
+    delete k;
+  }
   delete w;
 }
 
