@@ -21,6 +21,7 @@ thread_local std::string g_last_error;
 
 archead_status cuda_status(cudaError_t e) {
   g_last_error = cudaGetErrorString(e);
+  cudaGetLastError();  // (a later call's launch would be taken to have failed)
   return e == cudaErrorMemoryAllocation ? ARCHEAD_ERR_OOM : ARCHEAD_ERR_CUDA;
 }
 

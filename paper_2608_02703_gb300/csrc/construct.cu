@@ -561,6 +561,7 @@ namespace {
 
 archead_status fail_cuda(cudaError_t e) {
   set_last_error_message(cudaGetErrorString(e));
+  cudaGetLastError();  // (a later call's launch would be taken to have failed)
   return e == cudaErrorMemoryAllocation ? ARCHEAD_ERR_OOM : ARCHEAD_ERR_CUDA;
 }
 

@@ -92,6 +92,7 @@ extern "C" ARCHEAD_API archead_status archead_forward_decode_noalloc(archead_pac
   if (e == cudaSuccess) e = scratch_address(pack->device, &base);
   if (e != cudaSuccess) {
     set_last_error_message(cudaGetErrorString(e));
+    cudaGetLastError();  // (a later call's launch would be taken to have failed)
     return ARCHEAD_ERR_CUDA;
   }
   char *scratch = static_cast<char *>(base);
@@ -124,6 +125,7 @@ extern "C" ARCHEAD_API archead_status archead_forward_decode_noalloc(archead_pac
   if (e == cudaSuccess) e = launch_decode(dp, units < pack->sm_count ? units : pack->sm_count, s, pack->lr > 0);
   if (e != cudaSuccess) {
     set_last_error_message(cudaGetErrorString(e));
+    cudaGetLastError();  // (a later call's launch would be taken to have failed)
     return ARCHEAD_ERR_CUDA;
   }
   return ARCHEAD_OK;

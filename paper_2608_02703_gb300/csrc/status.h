@@ -12,6 +12,7 @@ void set_last_error_message(const char *msg);
 inline archead_status status_of(cudaError_t e) {
   if (e == cudaSuccess) return ARCHEAD_OK;
   set_last_error_message(cudaGetErrorString(e));
+  cudaGetLastError();  // (a later call's launch would be taken to have failed)
   return e == cudaErrorMemoryAllocation ? ARCHEAD_ERR_OOM : ARCHEAD_ERR_CUDA;
 }
 

@@ -92,3 +92,27 @@ def test_what_no_graph_holds_is_freed():
     archead.archead_int8_linear(w, x, 600, y)
     assert archead.archead_int8_device_bytes(w) == base - room + 600 * 4096 * 2 + (600 * 4 + 255) // 256 * 256
     w.close()
+
+
+def _too_much(w):
+    """A call whose scratch no device has (2^30 tokens of 1024 codes: 2 TB); nothing is queued."""
+    import torch
+
+    small = torch.zeros((1, w.K), device="cuda")
+    y = torch.zeros((1, w.N), device="cuda")
+    return archead.load().archead_int8_linear(w.handle, small.data_ptr(), archead.DTYPE_FP32, 1 << 30, w.K,
+                                              y.data_ptr(), archead.DTYPE_FP32, w.N, None)
+
+
+def test_a_failed_growth_is_the_failed_calls_alone():
+    import torch
+
+    w = _weight(256, 1024)
+    x, y = torch.randn((40, 1024), device="cuda"), torch.empty((40, 256), device="cuda")
+    archead.archead_int8_linear(w, x, 40, y)
+    want = y.clone()
+    assert _too_much(w) == archead.ERR_OOM
+    y.fill_(float("nan"))
+    archead.archead_int8_linear(w, x, 40, y)  # (not the failure of the call before)
+    assert archead.archead_int8_sync_status(w) == archead.OK and torch.equal(y, want)
+    w.close()
