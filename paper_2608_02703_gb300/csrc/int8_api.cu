@@ -86,8 +86,10 @@ cudaError_t grow_workspace(archead_int8_weight *w, size_t bytes) {
   w->ws = nullptr;
   w->ws_bytes = 0;
   w->ws_captured = false;
-  e = cudaMalloc(&w->ws, bytes);
-  if (e != cudaSuccess) return e;
+  w->reserved_tokens = 0;
+  void *ws = nullptr;
+  if ((e = cudaMalloc(&ws, bytes)) != cudaSuccess) return e;
+  w->ws = ws;
   w->ws_bytes = bytes;
   w->owned_bytes += (int64_t)bytes;
   return cudaSuccess;
@@ -98,16 +100,22 @@ archead_status ensure_workspace(archead_int8_weight *w, size_t bytes, int64_t M,
   const bool captured = is_capturing(s);
   if (captured && bytes <= w->ws_bytes) w->ws_captured = true;
   if (bytes <= w->ws_bytes && M <= w->reserved_tokens) return ARCHEAD_OK;
-  if (M > w->reserved_tokens && !captured) {
-    bytes = std::max(bytes, room_for(w, M));
-    w->reserved_tokens = M;
+  int64_t tokens = w->reserved_tokens;
+  if (M > tokens && !captured) {
+    tokens = std::max<int64_t>(M, kReserveTokens);  // (a growth that failed left nothing)
+    bytes = std::max(bytes, room_for(w, tokens));
   }
-  if (bytes <= w->ws_bytes) return ARCHEAD_OK;
+  if (bytes <= w->ws_bytes) {
+    w->reserved_tokens = tokens;
+    return ARCHEAD_OK;
+  }
   if (captured) {
     set_last_error_message("the workspace cannot grow while the stream is captured: call once with as many tokens before");
     return ARCHEAD_ERR_UNSUPPORTED;
   }
-  return status_of(grow_workspace(w, bytes));
+  const cudaError_t e = grow_workspace(w, bytes);
+  if (e == cudaSuccess) w->reserved_tokens = tokens;
+  return status_of(e);
 }
 
 template <typename T>
@@ -168,13 +176,13 @@ archead_status archead_int8_weight_create(const int8_t *codes, const float *scal
     w->K_pad = (int)((K + kI8PadK - 1) / kI8PadK * kI8PadK);
     w->wait_budget = kDefaultWaitBudget;
     if ((e = int8_gemm_room(w)) != cudaSuccess) return e;
-    w->reserved_tokens = kReserveTokens;
     const size_t code_bytes = (size_t)w->N_pad * w->K_pad, scale_bytes = (size_t)w->N_pad * sizeof(float);
     if ((e = cudaMalloc(&w->codes, code_bytes)) != cudaSuccess) return e;
     if ((e = cudaMalloc(&w->scales, scale_bytes)) != cudaSuccess) return e;
     if ((e = cudaMalloc(&w->err, 16)) != cudaSuccess) return e;
     w->owned_bytes = (int64_t)(code_bytes + scale_bytes + 16);
     if ((e = grow_workspace(w, room_for(w, kReserveTokens))) != cudaSuccess) return e;
+    w->reserved_tokens = kReserveTokens;
     if ((e = cudaMemsetAsync(w->err, 0, 16, s)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(w->scales, 0, scale_bytes, s)) != cudaSuccess) return e;
     if ((e = cudaMemcpyAsync(w->scales, scales, (size_t)N * sizeof(float), cudaMemcpyDefault, s)) != cudaSuccess)

@@ -116,3 +116,28 @@ def test_a_failed_growth_is_the_failed_calls_alone():
     archead.archead_int8_linear(w, x, 40, y)  # (not the failure of the call before)
     assert archead.archead_int8_sync_status(w) == archead.OK and torch.equal(y, want)
     w.close()
+
+
+def test_room_after_a_failed_growth():
+    """What a weight that could not grow has room for is what it says: a call leaves room for smaller ones again."""
+    import torch
+
+    w = _weight(256, 1024)
+    x, y = torch.randn((40, 1024), device="cuda"), torch.empty((40, 256), device="cuda")
+    archead.archead_int8_linear(w, x, 40, y)
+    want = y.clone()
+    new = archead.archead_int8_device_bytes(w)
+    assert _too_much(w) == archead.ERR_OOM
+    assert archead.archead_int8_device_bytes(w) < new
+    archead.archead_int8_linear(w, x, 20, y)
+    assert archead.archead_int8_device_bytes(w) == new  # (room for 64 tokens, as a new weight's)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        archead.archead_int8_linear(w, x, 40, y)
+    y.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+    graph.reset()
+    w.close()
