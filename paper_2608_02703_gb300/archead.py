@@ -415,10 +415,18 @@ class Int8Weight:
 
 
 def archead_int8_weight_create(codes, scales, stream=None) -> Int8Weight:
-    """codes int8 [N, K] and scales fp32 [N]: numpy arrays or torch tensors, on the host or the device."""
+    """codes int8 [N, K] and scales fp32 [N]: numpy arrays or torch tensors, on the host or the device.
+
+    Numpy codes of another type are taken where int8 holds them all."""
     N, K = codes.shape
     if isinstance(codes, np.ndarray):
-        codes = np.ascontiguousarray(codes, dtype=np.int8)
+        if codes.dtype != np.int8:
+            with np.errstate(invalid="ignore"):
+                same = codes.astype(np.int8)
+            if not np.array_equal(same, codes):
+                raise ValueError(f"codes of {codes.dtype} that int8 does not hold")
+            codes = same
+        codes = np.ascontiguousarray(codes)
         scales = np.ascontiguousarray(scales, dtype=np.float32)
         n_scales = scales.size
     else:
