@@ -385,9 +385,12 @@ def _rows(t, rows: int, cols: int, what: str) -> int:
     return stride[0] if shape[0] > 1 else cols
 
 
-def _flat(t, dtype, size: int, what: str):
-    """Address of a contiguous tensor of at least `size` elements of the type."""
-    if t.dtype is not dtype or t.numel() < size or not t.is_contiguous():
+def _flat(t, dtype, size: int, what: str, cols: Optional[int] = None):
+    """Address of a contiguous tensor of at least `size` elements of the type.  A matrix that is larger has rows of
+    `cols` elements: of others the wrong elements would be read or written."""
+    held = t.numel()
+    wider = held > size and cols is not None and t.dim() == 2 and t.shape[1] not in (1, cols)
+    if t.dtype is not dtype or held < size or wider or not t.is_contiguous():
         raise ValueError(f"{what}: {size} contiguous elements of {dtype} are wanted, not {tuple(t.shape)} of {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{what} is not on the GPU")
@@ -458,7 +461,7 @@ def archead_int8_quantize_tokens(x, codes, scales, stream=None) -> None:
 
     M, K = x.shape
     ldx = _rows(x, M, K, "x")
-    _check(load().archead_int8_quantize_tokens(x.data_ptr(), _dtype(x), M, K, ldx, _flat(codes, torch.int8, M * K, "codes"),
+    _check(load().archead_int8_quantize_tokens(x.data_ptr(), _dtype(x), M, K, ldx, _flat(codes, torch.int8, M * K, "codes", K),
                                                _flat(scales, torch.float32, M, "scales"), _stream_at(stream, x)),
            "archead_int8_quantize_tokens")
 
@@ -472,7 +475,7 @@ def archead_int8_matmul_path(weight: Int8Weight, x_codes, x_scales, M: int, y, p
     import torch
 
     ldy = _rows(y, M, weight.N, "y")
-    _check(load().archead_int8_matmul_path(weight.handle, _flat(x_codes, torch.int8, M * weight.K, "x_codes"),
+    _check(load().archead_int8_matmul_path(weight.handle, _flat(x_codes, torch.int8, M * weight.K, "x_codes", weight.K),
                                            _flat(x_scales, torch.float32, M, "x_scales"), M, y.data_ptr(), _dtype(y),
                                            ldy, path, _stream_at(stream, y)), "archead_int8_matmul")
 
@@ -537,10 +540,10 @@ def archead_beam_select(beam: Beam, logits, scores, out_scores, out_parents, out
     _check(load().archead_beam_select(
         beam.handle, logits.data_ptr(), _dtype(logits), batch, beams, vocab, ld,
         _flat(scores, torch.float32, batch * beams, "scores"),
-        None if ended is None else _flat(ended, torch.uint8, batch * beams, "ended"), end_token, n,
+        None if ended is None else _flat(ended, torch.uint8, batch * beams, "ended", beams), end_token, n,
         _flat(out_scores, torch.float32, batch * n, "out_scores"),
-        _flat(out_parents, torch.int32, batch * n, "out_parents"),
-        _flat(out_tokens, torch.int32, batch * n, "out_tokens"), _stream_at(stream, logits)), "archead_beam_select")
+        _flat(out_parents, torch.int32, batch * n, "out_parents", n),
+        _flat(out_tokens, torch.int32, batch * n, "out_tokens", n), _stream_at(stream, logits)), "archead_beam_select")
 
 
 def _merged(shape, strides, what: str):

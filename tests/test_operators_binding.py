@@ -45,3 +45,72 @@ def test_codes_that_int8_holds_are_taken(library, dtype):
     for given in (codes, np.asfortranarray(codes)):
         archead.archead_int8_weight_create(given, np.ones(2, np.float32), stream=0)
     assert len(library.calls) == 2
+
+
+class _OnGpu:
+    """A tensor of the host that says it is on the GPU (its address goes to the stand-in library only)."""
+
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 0
+
+    def view(self, *args):
+        return _OnGpu(self.t.view(*args))
+
+
+def _t(*shape, dtype="float32"):
+    import torch
+
+    return _OnGpu(torch.zeros(shape, dtype=getattr(torch, dtype)))
+
+
+def _quantize(**kw):
+    a = dict(x=_t(3, 6), codes=_t(3, 6, dtype="int8"), scales=_t(3)) | kw
+    archead.archead_int8_quantize_tokens(a["x"], a["codes"], a["scales"], stream=0)
+
+
+def _matmul(**kw):
+    a = dict(codes=_t(3, 6, dtype="int8"), scales=_t(3), M=3, y=_t(3, 10)) | kw
+    archead.archead_int8_matmul(archead.Int8Weight(None, 10, 6), a["codes"], a["scales"], a["M"], a["y"], stream=0)
+
+
+def _select(**kw):
+    a = dict(logits=_t(6, 9), scores=_t(2, 3), out_scores=_t(2, 4), out_parents=_t(2, 4, dtype="int32"),
+             out_tokens=_t(2, 4, dtype="int32"), ended=None) | kw
+    archead.archead_beam_select(archead.Beam(None), **a, stream=0)
+
+
+ELEMENTS = "contiguous elements"
+
+
+@pytest.mark.parametrize("call,kw", [
+    (_quantize, dict(codes=_t(3, 7, dtype="int8"))), (_quantize, dict(x=_t(3, 1), codes=_t(3, 6, dtype="int8"))),
+    (_matmul, dict(codes=_t(3, 8, dtype="int8"))), (_matmul, dict(codes=_t(4, 5, dtype="int8"))),
+    (_select, dict(out_parents=_t(2, 5, dtype="int32"))), (_select, dict(out_tokens=_t(3, 3, dtype="int32"))),
+    (_select, dict(ended=_t(2, 4, dtype="uint8"))),
+])
+def test_larger_matrices_of_other_rows_are_refused(library, call, kw):
+    with pytest.raises(ValueError, match=ELEMENTS):
+        call(**kw)
+    assert not library.calls
+
+
+@pytest.mark.parametrize("call,kw", [
+    (_quantize, dict()), (_quantize, dict(codes=_t(5, 6, dtype="int8"))), (_quantize, dict(codes=_t(100, dtype="int8"))),
+    (_quantize, dict(codes=_t(9, 2, dtype="int8"))), (_matmul, dict()), (_matmul, dict(codes=_t(4, 6, dtype="int8"))),
+    (_matmul, dict(codes=_t(3, 2, 3, dtype="int8"))), (_matmul, dict(M=0)), (_select, dict()),
+    (_select, dict(out_parents=_t(5, 4, dtype="int32"), out_tokens=_t(50, dtype="int32"))),
+    (_select, dict(ended=_t(2, 3, dtype="uint8"))), (_select, dict(ended=_t(2, 3, dtype="bool"))),
+    (_select, dict(ended=_t(4, 3, dtype="uint8"))),
+])
+def test_matrices_with_room_to_spare_are_taken(library, call, kw):
+    """More rows than the call needs, a flat buffer, or the same elements in another shape."""
+    call(**kw)
+    assert len(library.calls) == 1
