@@ -577,6 +577,9 @@ def archead_beam_state(t, row_dim: int = 0, length_dim: Optional[int] = None, ou
     if out is not None and (out.shape != t.shape or out.stride() != t.stride() or out.dtype != t.dtype):
         raise ValueError("out is not laid out as the state")
     shape, strides, size = list(t.shape), list(t.stride()), t.element_size()
+    for dim, what in ((row_dim, "rows"), (length_dim, "positions")):
+        if dim is not None and not -t.dim() <= dim < t.dim():
+            raise ValueError(f"a state of {t.dim()} dimensions has no dimension {dim} for its {what}")
     row_dim %= t.dim()
     if length_dim is None:
         # The dimensions that lie side by side at the end are one chunk.

@@ -114,3 +114,16 @@ def test_matrices_with_room_to_spare_are_taken(library, call, kw):
     """More rows than the call needs, a flat buffer, or the same elements in another shape."""
     call(**kw)
     assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("kw", [dict(row_dim=4), dict(row_dim=-5), dict(length_dim=4), dict(length_dim=-5)], ids=str)
+def test_dimensions_that_a_state_has_not_are_refused(kw):
+    import torch
+
+    t = torch.empty((2, 6, 8, 10))
+    with pytest.raises(ValueError, match="has no dimension"):
+        archead.archead_beam_state(t, **kw)
+    with pytest.raises(ValueError, match="has no dimension"):
+        archead.archead_beam_state(torch.tensor(1.0))
+    a, b = archead.archead_beam_state(t, row_dim=-3, length_dim=-2), archead.archead_beam_state(t, row_dim=1, length_dim=2)
+    assert (a.rows, a.room) == (b.rows, b.room) == (6, 8)
