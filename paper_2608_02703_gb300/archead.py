@@ -437,7 +437,14 @@ def archead_int8_weight_create(codes, scales, stream=None) -> Int8Weight:
 
         if codes.dtype != torch.int8 or scales.dtype != torch.float32:
             raise ValueError(f"codes in int8 and scales in fp32 are wanted, not {codes.dtype} and {scales.dtype}")
-        codes, scales = codes.contiguous(), scales.contiguous()
+        if not (codes.is_contiguous() and scales.is_contiguous()):
+            # Copied in the stream that the call reads in, behind what fills them there.
+            if stream is not None and (codes.is_cuda or scales.is_cuda):
+                given = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+            else:
+                given = None
+            with torch.cuda.stream(given):
+                codes, scales = codes.contiguous(), scales.contiguous()
         n_scales = scales.numel()
     if n_scales != N:
         raise ValueError(f"a scale for each of the {N} channels is wanted, not {n_scales}")

@@ -141,3 +141,36 @@ def test_room_after_a_failed_growth():
     assert torch.equal(y, want)
     graph.reset()
     w.close()
+
+
+@pytest.mark.parametrize("which", ["stream", "address", "default", "current"])
+def test_a_weight_of_strided_codes_filled_in_another_stream(which):
+    """Codes and scales that do not lie side by side are copied in the stream that the call was given."""
+    import torch
+
+    N, K, M = 96, 160, 3
+    g = torch.Generator(device="cuda").manual_seed(1)
+    wanted = torch.randint(-128, 128, (K, N), generator=g, device="cuda", dtype=torch.int8)
+    codes, scales = torch.zeros((K, N), dtype=torch.int8, device="cuda"), torch.zeros((N, 2), device="cuda")
+    x = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    side = torch.cuda.default_stream() if which == "default" else torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+        codes.copy_(wanted)
+        scales.fill_(1.0)
+
+    def create():
+        stream = dict(stream=side, address=side.cuda_stream, default=side, current=None)[which]
+        return archead.archead_int8_weight_create(codes.t(), scales[:, 0], stream=stream)
+
+    if which == "current":
+        with torch.cuda.stream(side):
+            w = create()
+    else:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            w = create()
+    y = torch.empty((M, N), device="cuda")
+    archead.archead_int8_matmul(w, x, torch.ones(M, device="cuda"), M, y)
+    assert torch.equal(y.double(), x.double() @ wanted.double())
+    w.close()
