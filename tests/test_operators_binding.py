@@ -1,7 +1,5 @@
 """The binding of the INT8 product and of beam search: each refusal is the one that is meant."""
 
-import ctypes
-
 import numpy as np
 import pytest
 
@@ -127,3 +125,98 @@ def test_dimensions_that_a_state_has_not_are_refused(kw):
         archead.archead_beam_state(torch.tensor(1.0))
     a, b = archead.archead_beam_state(t, row_dim=-3, length_dim=-2), archead.archead_beam_state(t, row_dim=1, length_dim=2)
     assert (a.rows, a.room) == (b.rows, b.room) == (6, 8)
+
+
+def _linear(**kw):
+    a = dict(x=_t(3, 6), M=3, y=_t(3, 10)) | kw
+    archead.archead_int8_linear(archead.Int8Weight(None, 10, 6), a["x"], a["M"], a["y"], stream=0)
+
+
+def _on_host(*shape, dtype="float32"):
+    return _t(*shape, dtype=dtype).t
+
+
+def _transposed(*shape, dtype="float32"):
+    return _OnGpu(_t(*shape, dtype=dtype).t.t())
+
+
+ROWS = "adjacent elements"
+HOST = "not on the GPU"
+TYPE = "bf16, fp16 or fp32"
+
+
+@pytest.mark.parametrize("call,kw,message", [
+    (_linear, dict(x=_t(3, 7)), ROWS), (_linear, dict(x=_t(2, 6)), ROWS), (_linear, dict(M=4), ROWS),
+    (_linear, dict(x=_t(18)), ROWS), (_linear, dict(x=_transposed(6, 3)), ROWS), (_linear, dict(y=_t(3, 9)), ROWS),
+    (_linear, dict(y=_transposed(10, 3)), ROWS), (_linear, dict(x=_t(3, 6, dtype="float64")), TYPE),
+    (_linear, dict(y=_t(3, 10, dtype="float64")), TYPE), (_linear, dict(y=_t(3, 10, dtype="int32")), TYPE),
+    (_linear, dict(x=_on_host(3, 6)), HOST), (_linear, dict(y=_on_host(3, 10)), HOST),
+    (_matmul, dict(codes=_t(3, 6)), ELEMENTS), (_matmul, dict(codes=_t(2, 6, dtype="int8")), ELEMENTS),
+    (_matmul, dict(codes=_transposed(6, 3, dtype="int8")), ELEMENTS), (_matmul, dict(scales=_t(2)), ELEMENTS),
+    (_matmul, dict(scales=_t(3, dtype="float64")), ELEMENTS), (_matmul, dict(y=_t(3, 11)), ROWS),
+    (_matmul, dict(M=4), ROWS), (_matmul, dict(y=_t(3, 10, dtype="int8")), TYPE),
+    (_matmul, dict(codes=_on_host(3, 6, dtype="int8")), HOST), (_matmul, dict(scales=_on_host(3)), HOST),
+    (_matmul, dict(y=_on_host(3, 10)), HOST),
+    (_quantize, dict(codes=_t(3, 6, dtype="uint8")), ELEMENTS), (_quantize, dict(codes=_t(2, 6, dtype="int8")), ELEMENTS),
+    (_quantize, dict(scales=_t(2)), ELEMENTS), (_quantize, dict(x=_transposed(6, 3)), ROWS),
+    (_quantize, dict(x=_t(3, 6, dtype="int32")), TYPE), (_quantize, dict(x=_on_host(3, 6)), HOST),
+    (_quantize, dict(codes=_on_host(3, 6, dtype="int8")), HOST), (_quantize, dict(scales=_on_host(3)), HOST),
+    (_select, dict(logits=_t(5, 9)), ROWS), (_select, dict(logits=_transposed(9, 6)), ROWS),
+    (_select, dict(logits=_t(6, 9, dtype="float64")), TYPE), (_select, dict(scores=_t(2, 3, dtype="float64")), ELEMENTS),
+    (_select, dict(scores=_transposed(3, 2)), ELEMENTS), (_select, dict(scores=_t(3, 3)), ROWS),
+    (_select, dict(out_scores=_t(2, 4, dtype="float16")), ELEMENTS), (_select, dict(out_scores=_t(1, 4)), ELEMENTS),
+    (_select, dict(out_scores=_t(2, 5)), ELEMENTS), (_select, dict(out_parents=_t(2, 4, dtype="int64")), ELEMENTS),
+    (_select, dict(out_parents=_t(1, 4, dtype="int32")), ELEMENTS), (_select, dict(out_tokens=_t(2, 4)), ELEMENTS),
+    (_select, dict(out_tokens=_t(2, 3, dtype="int32")), ELEMENTS), (_select, dict(ended=_t(2, 2, dtype="uint8")), ELEMENTS),
+    (_select, dict(ended=_t(2, 3, dtype="int32")), ELEMENTS), (_select, dict(logits=_on_host(6, 9)), HOST),
+    (_select, dict(scores=_on_host(2, 3)), HOST), (_select, dict(ended=_on_host(2, 3, dtype="uint8")), HOST),
+    (_select, dict(out_scores=_on_host(2, 4)), HOST), (_select, dict(out_tokens=_on_host(2, 4, dtype="int32")), HOST),
+])
+def test_one_wrong_argument_is_refused_for_what_is_wrong(library, call, kw, message):
+    call()
+    assert len(library.calls) == 1  # the same call with the right argument
+    with pytest.raises(ValueError, match=message):
+        call(**kw)
+    assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("codes,scales,message", [
+    (np.zeros((3, 4), np.int8), np.zeros(4, np.float32), "a scale for each"),
+    (_on_host(3, 4), _on_host(3), "codes in int8"), (_on_host(3, 4, dtype="int8"), _on_host(3, dtype="float64"), "codes in int8"),
+    (_on_host(3, 4, dtype="int8"), _on_host(4), "a scale for each"),
+])
+def test_weights_are_refused_for_what_is_wrong(library, codes, scales, message):
+    with pytest.raises(ValueError, match=message):
+        archead.archead_int8_weight_create(codes, scales, stream=0)
+    assert not library.calls
+    archead.archead_int8_weight_create(_on_host(3, 4, dtype="int8"), _on_host(3), stream=0)
+    assert len(library.calls) == 1
+
+
+def _reorder(states, parents, length):
+    archead.archead_beam_reorder(states, parents, length, stream=0)
+
+
+def test_reorderings_are_refused_for_what_is_wrong(library):
+    def states(*t):
+        s = archead.archead_beam_states([archead.archead_beam_state(a, length_dim=2) for a in t])
+        s.on_gpu = True
+        return s
+
+    cache, parents = _on_host(4, 6, 8, 10), _t(2, 2, dtype="int32")
+    good = states(cache, cache)
+    _reorder(good, parents, 8)
+    assert len(library.calls) == 1
+    _, args = library.calls[0]
+    assert args[1:3] == (2, parents.data_ptr()) and args[3:6] == (2, 2, 8)
+    for bad, message in ((lambda: _reorder(good, parents, 9), "positions"),
+                         (lambda: _reorder(good, _t(3, 2, dtype="int32"), 8), "rows"),
+                         (lambda: _reorder(states(cache, cache[:3]), parents, 8), "rows"),
+                         (lambda: _reorder(good, _t(2, 2, dtype="int64"), 8), ELEMENTS),
+                         (lambda: _reorder(good, _transposed(2, 2, dtype="int32"), 8), ELEMENTS),
+                         (lambda: _reorder(good, _on_host(2, 2, dtype="int32"), 8), HOST),
+                         (lambda: _reorder(archead.archead_beam_states([archead.archead_beam_state(cache)]), parents, 8),
+                          "a state is not on the GPU")):
+        with pytest.raises(ValueError, match=message):
+            bad()
+    assert len(library.calls) == 1
