@@ -59,13 +59,6 @@ struct Raw8 {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool vec, int64_t left, float (&v)[8]) {
-  Raw8<T> r;
-  r.load(p, vec, left);
-  r.values(v);
-}
-
 // A running maximum of |v| whose NaNs stay; its bits order as the values do, a
 // NaN above infinity.
 __device__ __forceinline__ float abs_max(float a, float b) {
