@@ -30,7 +30,10 @@
  *    device before freeing the old one, so earlier calls on any stream are
  *    done with it.  A call that is not being captured leaves room for every
  *    AUTO call of its kind (logits; or cross entropy, greedy and partials)
- *    with fewer tokens.  Different packs are independent.
+ *    with fewer tokens.  A captured forward holds that workspace: capture
+ *    after a call with the most tokens that the pack will see, and replay no
+ *    graph from before a call that needed more.  Different packs are
+ *    independent.
  *  - Faults detected on the device (an out-of-range target, a pipeline wait
  *    that gave up) are latched in a per-pack device error word and reported
  *    by archead_sync_status().
@@ -443,7 +446,8 @@ ARCHEAD_API archead_status archead_dequant_residual_sc4(const int8_t *codes, con
  *   ARCHEAD_PATH_PREFILL the tensor-memory kernel.
  * archead_int8_sync_status: waits for the stream, then reads and clears the
  *   weight's device error word (ARCHEAD_ERR_DEVICE_TIMEOUT: a pipeline wait
- *   gave up).  archead_int8_set_wait_budget: as archead_set_wait_budget.
+ *   gave up, and what the call wrote is not to be used; the weight is as good
+ *   as before).  archead_int8_set_wait_budget: as archead_set_wait_budget.
  * archead_int8_device_bytes: device memory the weight holds now (-1: NULL).
  */
 typedef struct archead_int8_weight archead_int8_weight; /* opaque, owned by the library */

@@ -21,8 +21,9 @@
 //   - epilogue warps read the accumulators, scale, round and store.
 //
 // Bound: by the tensor cores from some 200 tokens on (512 tokens of 151936 x 4096
-// 343 us, 2048 1.42 ms: 96% of the rate that the library's bf16 product reaches), by
-// memory for fewer of a large weight (64 tokens 100 us, 128 105: 93%), and by its
+// 338 us, 2048 1.32 ms: all of the rate that the library's bf16 product reaches in a
+// burst; at the power limit 375 us and 1.40 to 1.44 ms), by memory for fewer of a
+// large weight (64 tokens 99 us, 128 106: 95 and 92%), and by its
 // start, its stages' pace and its join for a small weight (64 tokens of 4096 x 512
 // 5.7 us, the quantiser's launch included).
 #include <cuda_fp16.h>
