@@ -131,8 +131,6 @@ def prepare(case, seed):
             s["y"] = torch.empty((M, d), dtype=_DTYPES[case["y"]], device="cuda") if case["y"] else None
             s["codes"] = torch.empty((M, d), dtype=torch.int8, device="cuda") if case["codes"] else None
             s["scales"] = torch.empty(M, dtype=torch.float32, device="cuda") if case["codes"] else None
-            if own and case["codes"]:
-                s["values"], s["column"] = torch.empty((M, d), dtype=torch.float32, device="cuda"), s["scales"][:, None]
         else:
             s["h"] = _hidden(gen, M, d).to(dtype)
             s["dy"] = (torch.randn((M, d), generator=gen, device="cuda") / d).to(dtype)
@@ -247,7 +245,7 @@ def _own(s, case):
                              codes=s["codes"], scales=s["scales"])
         out = {k: s[k] for k in ("sum", "y", "scales") if s[k] is not None}
         if s["codes"] is not None:
-            out["values"] = torch.mul(s["codes"], s["column"], out=s["values"])
+            out["values"] = s["codes"].float() * s["scales"][:, None]
         return out
     if op == "norm_grad":
         lib.archead_rms_norm_backward(s["norm"], s["dy"], s["h"], s["weight"], s["rstd"], s["dx"],
