@@ -12,6 +12,7 @@
 
 #include "device.cuh"
 #include "internal.h"
+#include "status.h"
 
 using namespace archead;
 
@@ -744,10 +745,8 @@ archead_status archead_sync_status(archead_pack *pack, void *stream) {
   if (!pack) return ARCHEAD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_CUDA(cudaSetDevice(pack->device));
-  AH_CUDA(cudaStreamSynchronize(s));
   int word = 0;
-  AH_CUDA(cudaMemcpy(&word, pack->err, sizeof(int), cudaMemcpyDeviceToHost));
-  AH_CUDA(cudaMemset(pack->err, 0, sizeof(int)));
+  AH_CUDA(take_error_word(pack->err, s, &word));
   if (word & kErrWaitTimeout) return ARCHEAD_ERR_DEVICE_TIMEOUT;
   if (word & kErrTargetRange) return ARCHEAD_ERR_TARGET_RANGE;
   if (word & kErrLayout) {

@@ -274,11 +274,8 @@ archead_status archead_int8_sync_status(archead_int8_weight *w, void *stream) {
   if (!w) return ARCHEAD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_TRY(cudaSetDevice(w->device));
-  AH_TRY(cudaStreamSynchronize(s));
   int word = 0;
-  AH_TRY(cudaMemcpyAsync(&word, w->err, sizeof(int), cudaMemcpyDeviceToHost, s));
-  AH_TRY(cudaStreamSynchronize(s));
-  AH_TRY(cudaMemsetAsync(w->err, 0, sizeof(int), s));
+  AH_TRY(take_error_word(w->err, s, &word));
   if (word & kErrLayout) {
     set_last_error_message("a kernel found its shared-memory window misaligned for its TMA layout and skipped its work");
     return ARCHEAD_ERR_UNSUPPORTED;

@@ -261,11 +261,8 @@ archead_status archead_loss_sync_status(archead_loss *l, void *stream) {
   if (!l) return ARCHEAD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   AH_TRY(cudaSetDevice(l->device));
-  AH_TRY(cudaStreamSynchronize(s));
   int word = 0;
-  AH_TRY(cudaMemcpyAsync(&word, l->err, sizeof(int), cudaMemcpyDeviceToHost, s));
-  AH_TRY(cudaStreamSynchronize(s));
-  AH_TRY(cudaMemsetAsync(l->err, 0, sizeof(int), s));
+  AH_TRY(take_error_word(l->err, s, &word));
   if (word & kErrLayout) return refuse("a kernel found its shared-memory window misaligned for its TMA layout and skipped its work");
   if (word & kErrWaitTimeout) return ARCHEAD_ERR_DEVICE_TIMEOUT;
   return word & kErrTargetRange ? ARCHEAD_ERR_TARGET_RANGE : ARCHEAD_OK;
