@@ -47,7 +47,8 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kAcc = 2;                              // accumulators of 256 columns
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 128 + 32 * kEpiWarps;
-constexpr int kSegment = 16;                         // steps of a sum of l in tensor memory (kLoss)
+// Steps of a sum in tensor memory where it is taken in parts, which epilogue warps add in registers.
+constexpr int kSegment = 16;
 constexpr int kBoxBytes = 32 * 64 * 2;               // outputs that a warp stages: 32 rows of 64 columns
 // The gradient's outputs of few tokens are bound by what leaves: there a warp fills a box while its last one is read.
 // The loss has no boxes, and epilogue warps that hold a unit's sums in registers.
@@ -59,9 +60,10 @@ struct Geom {
   static constexpr int kBarOff = kOutOff + kEpiWarps * kBoxes * kBoxBytes;
   static constexpr int kBars = 2 * kStages + 2 * kAcc + 1;
   static constexpr int kSmem = kBarOff + kBars * 8 + 32 + 16;
-  // kLoss: registers of the loading warpgroup and of the others, whose sum is at most that of the launch.
+  // Sums in parts: registers of the loading warpgroup and of the others, whose sum is at most that of the launch.
   static constexpr int kRegs0 = 56, kRegsE = 216;
-  static_assert(128 * kRegs0 + 32 * kEpiWarps * kRegsE <= 65536 / kThreads / 8 * 8 * kThreads, "registers");
+  static constexpr int kRegsInAll = 128 * kRegs0 + 32 * kEpiWarps * kRegsE;
+  static_assert(kRegsInAll <= 65536 / kThreads / 8 * 8 * kThreads, "registers");
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static_assert(kStages <= 16, "kinds of the stages");
 };
@@ -340,20 +342,22 @@ __device__ __forceinline__ void sum_columns(float (&v)[32], int64_t base, int64_
   sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
 }
 
-// A half's columns of an accumulator's row, every other 32, added to what is held (or put there).
-__device__ __forceinline__ void add_columns(uint32_t taddr, int half, int chunks, bool put, float (&held)[4][32]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (half + 2 * i < chunks) {
-      float v[32];
-      read_columns<32>(taddr + 32 * (half + 2 * i), v);
-#pragma unroll
-      for (int j = 0; j < 32; ++j) held[i][j] = put ? v[j] : held[i][j] + v[j];
-    }
-  }
+// The i-th 32 columns of a half: every other 32 of the unit (kLoss), or every other 64 (kSoftmax: a box's).
+template <Mode kMode>
+__device__ __forceinline__ int chunk_of(int half, int i) {
+  return kMode == kLoss ? half + 2 * i : 2 * half + (i & 1) + 4 * (i >> 1);
 }
 
-template <Mode kMode>
+// 32 columns of an accumulator's row added to what is held.
+__device__ __forceinline__ void add_columns(uint32_t taddr, float (&held)[32]) {
+  float v[32];
+  read_columns<32>(taddr, v);
+#pragma unroll
+  for (int j = 0; j < 32; ++j) held[j] += v[j];
+}
+
+// kParts: sums over more than a segment are taken in parts.
+template <Mode kMode, bool kParts>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     linear_ce_kernel(const __grid_constant__ Params p) {
   using G = Geom<kMode>;
@@ -461,7 +465,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   Units<kMode> units(p, count);
 
   if (warp < 4) {
-    if (kMode == kLoss) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegs0) : "memory");
+    if (kParts) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(G::kRegs0) : "memory");
     if (warp == 0) {
       // ------------------------------ loads ------------------------------
       const bool one = elect_one();
@@ -505,7 +509,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t a_step = a_outer ? 2048 >> 4 : 32 >> 4, b_step = b_outer ? 2048 >> 4 : 32 >> 4;  // 16 of the sum
         int k = u.k0;
         do {
-          const int end = kMode == kLoss ? min(u.k1, k + kSegment) : u.k1;
+          const int end = kParts ? min(u.k1, k + kSegment) : u.k1;
           if (!mbar_wait_warp(&acc_empty[acc.s], acc.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
             stop = true;
             break;
@@ -539,7 +543,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else {
     // ------------------------------ epilogue ------------------------------
-    if (kMode == kLoss) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(G::kRegsE) : "memory");
+    if (kParts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(G::kRegsE) : "memory");
     const int quad = warp & 3, half = (warp - 4) >> 2;
     OutBox<G::kBoxes> box{smem_u32(smem) + G::kOutOff + (warp - 4) * G::kBoxes * kBoxBytes, lane};
     const uint32_t taddr0 = tmem_base + ((uint32_t)(quad * 32) << 16) + (kMode == kGrad ? 128 * half : 0);
@@ -560,15 +564,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int64_t row0 = row - lane;
       // The sum of l over a segment: tensor cores round its additions toward zero, by up to 2^-23 of the
       // sum so far each, and always so.  Sums of up to 1024 products are added to one another here (2048 tokens x
-      // 151936 x 4096: the loss in error by 4e-7 of itself, in one sum 1.6e-6).
-      float held[kMode == kLoss ? 4 : 1][32];
+      // 151936 x 4096: the loss in error by 4e-7 of itself, in one sum 1.6e-6).  G takes l in the same parts as the loss
+      // that its lse comes from: of a target that the model is sure of, 1 - p is as small as what l would differ by (1e-4
+      // for l = 20 of 4096 products in one sum).
+      float held[kParts ? 4 : 1][32] = {};
+      // (G's rows up to a whole stage are read as dW's summed dimension; rows past the tokens that count are zeros
+      // there, and of no account in dx.)
+      const int needed = kMode == kSoftmax ? (count + kCeStep - 1) / kCeStep * kCeStep : count;
       bool stop = false;
-      if constexpr (kMode == kLoss) {
-        for (int k = 0; k + kSegment < u.k1 && !stop; k += kSegment) {
+      if constexpr (kParts) {
+        for (int k = u.k0; k + kSegment < u.k1 && !stop; k += kSegment) {
           stop = !mbar_wait_warp(&acc_full[acc.s], acc.ph, p.wait_budget, abort_flag, p.err);
           if (stop) break;
           tc_fence_after();
-          if (row0 < count) add_columns(taddr0 + acc.s * kCeTile, half, p.nt / 32, k == 0, held);
+          if (row0 < needed) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int c = chunk_of<kMode>(half, i);
+              if (c < p.nt / 32) add_columns(taddr0 + acc.s * kCeTile + 32 * c, held[i]);
+            }
+          }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) arrive_cluster(of_rank(smem_u32(&acc_empty[acc.s]), 0));
@@ -582,29 +597,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int64_t col0 = (int64_t)u.col * p.nt;
         if (!through) m = -INFINITY, sum = 0.f;
         if (row0 < count) {
-          add_columns(taddr, half, p.nt / 32, u.k1 <= kSegment, held);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int c = half + 2 * i;
-            if (c < p.nt / 32) sum_columns(held[i], col0 + 32 * c, p.V, t, &p.at.tlogit[row], m, sum);
+            const int c = chunk_of<kMode>(half, i);
+            if (c < p.nt / 32) {
+              add_columns(taddr + 32 * c, held[i]);
+              sum_columns(held[i], col0 + 32 * c, p.V, t, &p.at.tlogit[row], m, sum);
+            }
           }
           if (live && !through) p.at.part[((int64_t)u.col * kCeParts + half) * p.rows + row] = make_float2(m, sum);
           if (live) last_row = row;
         }
       } else if constexpr (kMode == kSoftmax) {
-        // G's rows up to a whole stage are read as dW's summed dimension; rows past the tokens that
-        // count are zeros there, and of no account in dx.
         const int64_t col0 = p.first_tile * kCeTile + u.col * p.nt;
-        if (row0 < (count + kCeStep - 1) / kCeStep * kCeStep) {
+        if (row0 < needed) {
           const float minus = -lse;
           const float2 f2 = make_float2(f, f);
           const bool all_live = __all_sync(0xffffffffu, live);
-          Columns32 next(taddr + 64 * half);
-#pragma unroll 1
-          for (int c = 2 * half; c < p.nt / 32; c += c & 1 ? 3 : 1) {  // (every other 64 columns)
-            float v[32];
-            const int after = c + (c & 1 ? 3 : 1);
-            next.take(v, taddr + 32 * after, after < p.nt / 32);
+          const auto softmax = [&](float (&v)[32], int c) {
             const int64_t base = col0 + 32 * c;
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
@@ -631,6 +641,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               box.put((c & 1) * 4 + j / 8, pack_out(v[j], v[j + 1], p.fp16), pack_out(v[j + 2], v[j + 3], p.fp16),
                       pack_out(v[j + 4], v[j + 5], p.fp16), pack_out(v[j + 6], v[j + 7], p.fp16));
             if (c & 1) box.store(&p.out, 0, (u.col * p.nt + 32 * c) / 64 * (int)p.rows + (int)row0);
+          };
+          if constexpr (kParts) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int c = chunk_of<kMode>(half, i);
+              if (c < p.nt / 32) {
+                add_columns(taddr + 32 * c, held[i]);
+                softmax(held[i], c);
+              }
+            }
+          } else {
+            Columns32 next(taddr + 64 * half);
+#pragma unroll 1
+            for (int c = 2 * half; c < p.nt / 32; c += c & 1 ? 3 : 1) {  // (as chunk_of)
+              float v[32];
+              const int after = c + (c & 1 ? 3 : 1);
+              next.take(v, taddr + 32 * after, after < p.nt / 32);
+              softmax(v, c);
+            }
           }
         }
       } else {
@@ -791,9 +820,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-template <Mode kMode>
+template <Mode kMode, bool kParts>
 cudaError_t launch(const Params &p, int64_t units, int clusters, cudaStream_t s) {
-  auto kern = linear_ce_kernel<kMode>;
+  auto kern = linear_ce_kernel<kMode, kParts>;
   cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), Geom<kMode>::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -865,11 +894,20 @@ int64_t logits_units(const CeCall &c, const Params &p) {
 
 }  // namespace
 
+// (A block that was launched with fewer registers than it hands on would wait for them.)
+template <Mode kMode>
+static cudaError_t registers_do() {
+  cudaFuncAttributes a;
+  const cudaError_t e = cudaFuncGetAttributes(&a, linear_ce_kernel<kMode, true>);
+  return e != cudaSuccess ? e : a.numRegs * kThreads < Geom<kMode>::kRegsInAll ? cudaErrorInvalidConfiguration : cudaSuccess;
+}
+
 cudaError_t ce_clusters(int *clusters) {
-  auto kern = linear_ce_kernel<kLoss>;
+  auto kern = linear_ce_kernel<kLoss, true>;
   constexpr int kSmem = Geom<kLoss>::kSmem;
   cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), kSmem);
   if (e != cudaSuccess) return e;
+  if ((e = registers_do<kLoss>()) != cudaSuccess || (e = registers_do<kSoftmax>()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
   cfg.blockDim = dim3(kThreads);
@@ -893,7 +931,7 @@ cudaError_t launch_ce_logits(const CeCall &c, CeParts *parts, cudaStream_t s) {
   const int64_t units = logits_units(c, p), columns = (c.V + p.nt - 1) / p.nt;
   parts->by_tile = (int)columns * kCeParts;
   parts->by_pair = (int)std::min<int64_t>({units, columns, c.loss->clusters}) * kCeParts;
-  return launch<kLoss>(p, units, c.loss->clusters, s);
+  return launch<kLoss, true>(p, units, c.loss->clusters, s);
 }
 
 int64_t ce_piece_tiles(const archead_loss *l, const CeCall &c) {
@@ -936,11 +974,13 @@ cudaError_t launch_ce_gradient(const CeCall &c, cudaStream_t s) {
   for (int64_t first = 0; first < tiles; first += per) {
     p.first_tile = g.first_tile = first;
     p.tiles = g.tiles = (int)std::min(per, tiles - first);
-    cudaError_t e = launch<kSoftmax>(p, logits_units(c, p), c.loss->clusters, s);
+    const int64_t of_g = logits_units(c, p);
+    cudaError_t e = c.d > kSegment * kCeStep ? launch<kSoftmax, true>(p, of_g, c.loss->clusters, s)
+                                             : launch<kSoftmax, false>(p, of_g, c.loss->clusters, s);
     if (e != cudaSuccess) return e;
     g.add_dx = first > 0;
     const int64_t units = (g.want_dx ? nm * nd * g.splits : 0) + (g.want_dw ? g.tiles * nd : 0);
-    if ((e = launch<kGrad>(g, units, c.loss->clusters, s)) != cudaSuccess) return e;
+    if ((e = launch<kGrad, false>(g, units, c.loss->clusters, s)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
