@@ -47,8 +47,11 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kAcc = 2;                              // accumulators of 256 columns
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 128 + 32 * kEpiWarps;
-// Steps of a sum in tensor memory where it is taken in parts, which epilogue warps add in registers.
-constexpr int kSegment = 16;
+// Steps of a sum in tensor memory where it is taken in parts, which epilogue warps add in registers: of a logit, and of
+// an element of dx or dW.  Tensor cores round their additions toward zero, by up to 2^-23 of the sum so far each, and
+// always so.  For a logit see the epilogue; of a gradient's terms of one sign 8192 lose some 2^-15 in this way (in one
+// sum 2^18 lost 1.2e-3, more than fp16's rounding).
+constexpr int kSegment = 16, kGradSegment = 128;
 constexpr int kBoxBytes = 32 * 64 * 2;               // outputs that a warp stages: 32 rows of 64 columns
 // The gradient's outputs of few tokens are bound by what leaves: there a warp fills a box while its last one is read.
 // The loss has no boxes, and epilogue warps that hold a unit's sums in registers.
@@ -342,10 +345,10 @@ __device__ __forceinline__ void sum_columns(float (&v)[32], int64_t base, int64_
   sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
 }
 
-// The i-th 32 columns of a half: every other 32 of the unit (kLoss), or every other 64 (kSoftmax: a box's).
+// The i-th 32 columns of a half: every other 32 of the unit (kLoss), every other 64 (kSoftmax: a box's), or 128 (kGrad).
 template <Mode kMode>
 __device__ __forceinline__ int chunk_of(int half, int i) {
-  return kMode == kLoss ? half + 2 * i : 2 * half + (i & 1) + 4 * (i >> 1);
+  return kMode == kLoss ? half + 2 * i : kMode == kSoftmax ? 2 * half + (i & 1) + 4 * (i >> 1) : 4 * half + i;
 }
 
 // 32 columns of an accumulator's row added to what is held.
@@ -361,7 +364,7 @@ template <Mode kMode, bool kParts>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     linear_ce_kernel(const __grid_constant__ Params p) {
   using G = Geom<kMode>;
-  constexpr int kStages = G::kStages;
+  constexpr int kStages = G::kStages, kPart = kMode == kGrad ? kGradSegment : kSegment;
   extern __shared__ uint8_t smem[];  // 1024-byte aligned (the swizzle's period)
   uint64_t *full = reinterpret_cast<uint64_t *>(smem + G::kBarOff), *empty = full + kStages;
   uint64_t *acc_full = empty + kStages, *acc_empty = acc_full + kAcc, *drain = acc_empty + kAcc;
@@ -509,7 +512,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t a_step = a_outer ? 2048 >> 4 : 32 >> 4, b_step = b_outer ? 2048 >> 4 : 32 >> 4;  // 16 of the sum
         int k = u.k0;
         do {
-          const int end = kParts ? min(u.k1, k + kSegment) : u.k1;
+          const int end = kParts ? min(u.k1, k + kPart) : u.k1;
           if (!mbar_wait_warp(&acc_empty[acc.s], acc.ph ^ 1, p.wait_budget, abort_flag, p.err)) {
             stop = true;
             break;
@@ -546,7 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (kParts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(G::kRegsE) : "memory");
     const int quad = warp & 3, half = (warp - 4) >> 2;
     OutBox<G::kBoxes> box{smem_u32(smem) + G::kOutOff + (warp - 4) * G::kBoxes * kBoxBytes, lane};
-    const uint32_t taddr0 = tmem_base + ((uint32_t)(quad * 32) << 16) + (kMode == kGrad ? 128 * half : 0);
+    const uint32_t taddr0 = tmem_base + ((uint32_t)(quad * 32) << 16);
     // With one row of tiles a token's sum goes on over all of this pair's units.
     const bool through = kMode == kLoss && count <= kCeTile;
     float m = -INFINITY, sum = 0.f;
@@ -567,27 +570,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // 151936 x 4096: the loss in error by 4e-7 of itself, in one sum 1.6e-6).  G takes l in the same parts as the loss
       // that its lse comes from: of a target that the model is sure of, 1 - p is as small as what l would differ by (1e-4
       // for l = 20 of 4096 products in one sum).
-      float held[kParts ? 4 : 1][32] = {};
       // (G's rows up to a whole stage are read as dW's summed dimension; rows past the tokens that count are zeros
       // there, and of no account in dx.)
       const int needed = kMode == kSoftmax ? (count + kCeStep - 1) / kCeStep * kCeStep : count;
-      bool stop = false;
-      if constexpr (kParts) {
-        for (int k = u.k0; k + kSegment < u.k1 && !stop; k += kSegment) {
-          stop = !mbar_wait_warp(&acc_full[acc.s], acc.ph, p.wait_budget, abort_flag, p.err);
-          if (stop) break;
+      const bool wanted = kMode == kGrad && u.dw ? p.first_tile * kCeTile + row0 < p.V : row0 < needed;
+      const int chunks = kMode == kGrad ? kCeTile / 32 : p.nt / 32;
+      // The sum of all parts but the last.
+      const auto add_parts = [&](float (&held)[4][32]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) held[i][j] = 0.f;
+        for (int k = u.k0; k + kPart < u.k1; k += kPart) {
+          if (!mbar_wait_warp(&acc_full[acc.s], acc.ph, p.wait_budget, abort_flag, p.err)) return false;
           tc_fence_after();
-          if (row0 < needed) {
+          if (wanted) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int c = chunk_of<kMode>(half, i);
-              if (c < p.nt / 32) add_columns(taddr0 + acc.s * kCeTile + 32 * c, held[i]);
+              if (c < chunks) add_columns(taddr0 + acc.s * kCeTile + 32 * c, held[i]);
             }
           }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) arrive_cluster(of_rank(smem_u32(&acc_empty[acc.s]), 0));
           acc.next();
+        }
+        return true;
+      };
+      float held[kParts && kMode != kGrad ? 4 : 1][32];
+      bool stop = false;
+      if constexpr (kParts && kMode != kGrad) {
+        stop = !add_parts(held);
+      } else if constexpr (kParts) {
+        if (u.k1 - u.k0 > kPart) {  // the whole sums take the last part's place, and go on as those of one part do
+          float sums[4][32];
+          stop = !add_parts(sums) || !mbar_wait_warp(&acc_full[acc.s], acc.ph, p.wait_budget, abort_flag, p.err);
+          if (!stop && wanted) {
+            tc_fence_after();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t at = taddr0 + acc.s * kCeTile + 32 * chunk_of<kMode>(half, i);
+              add_columns(at, sums[i]);
+              tmem_st32(at, sums[i]);
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+          }
         }
       }
       if (stop || !mbar_wait_warp(&acc_full[acc.s], acc.ph, p.wait_budget, abort_flag, p.err)) break;
@@ -596,11 +624,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       if constexpr (kMode == kLoss) {
         const int64_t col0 = (int64_t)u.col * p.nt;
         if (!through) m = -INFINITY, sum = 0.f;
-        if (row0 < count) {
+        if (wanted) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int c = chunk_of<kMode>(half, i);
-            if (c < p.nt / 32) {
+            if (c < chunks) {
               add_columns(taddr + 32 * c, held[i]);
               sum_columns(held[i], col0 + 32 * c, p.V, t, &p.at.tlogit[row], m, sum);
             }
@@ -610,7 +638,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       } else if constexpr (kMode == kSoftmax) {
         const int64_t col0 = p.first_tile * kCeTile + u.col * p.nt;
-        if (row0 < needed) {
+        if (wanted) {
           const float minus = -lse;
           const float2 f2 = make_float2(f, f);
           const bool all_live = __all_sync(0xffffffffu, live);
@@ -646,7 +674,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int c = chunk_of<kMode>(half, i);
-              if (c < p.nt / 32) {
+              if (c < chunks) {
                 add_columns(taddr + 32 * c, held[i]);
                 softmax(held[i], c);
               }
@@ -654,10 +682,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           } else {
             Columns32 next(taddr + 64 * half);
 #pragma unroll 1
-            for (int c = 2 * half; c < p.nt / 32; c += c & 1 ? 3 : 1) {  // (as chunk_of)
+            for (int c = 2 * half; c < chunks; c += c & 1 ? 3 : 1) {  // (as chunk_of)
               float v[32];
               const int after = c + (c & 1 ? 3 : 1);
-              next.take(v, taddr + 32 * after, after < p.nt / 32);
+              next.take(v, taddr + 32 * after, after < chunks);
               softmax(v, c);
             }
           }
@@ -665,13 +693,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       } else {
         const int64_t col0 = (int64_t)u.col * kCeTile + 128 * half;
         const int64_t n0 = p.first_tile * kCeTile + row0;
+        const uint32_t mine = taddr + 128 * half;
         if (u.dw && p.box_out) {
 #pragma unroll 1
           for (int c = 0; c < 2; ++c) {
-            if (n0 >= p.V || col0 + 64 * c >= p.d) break;  // (the same for the warp)
+            if (!wanted || col0 + 64 * c >= p.d) break;  // (the same for the warp)
             float v[64];
             if (u.k1 > u.k0) {
-              read_columns<64>(taddr + 64 * c, v);
+              read_columns<64>(mine + 64 * c, v);
             } else {
 #pragma unroll
               for (int j = 0; j < 64; ++j) v[j] = 0.f;
@@ -688,11 +717,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             box.store(&p.out, (int)(col0 + 64 * c), (int)n0);
           }
         } else if (!u.dw && !p.add_dx) {
-          if (row0 < count) {  // (rows past the tokens that count are never read)
+          if (wanted) {  // (rows past the tokens that count are never read)
 #pragma unroll 1
             for (int c = 0; c < 4 && col0 + 32 * c < p.d; ++c) {
               float v[32];
-              read_columns<32>(taddr + 32 * c, v);
+              read_columns<32>(mine + 32 * c, v);
               box.begin();
 #pragma unroll
               for (int j = 0; j < 8; ++j)
@@ -708,7 +737,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const int64_t base = col0 + 32 * c;
           __syncwarp();
           if (u.k1 > u.k0) {
-            read_columns<32>(taddr + 32 * c, v);
+            read_columns<32>(mine + 32 * c, v);
           } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = 0.f;
@@ -907,7 +936,9 @@ cudaError_t ce_clusters(int *clusters) {
   constexpr int kSmem = Geom<kLoss>::kSmem;
   cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), kSmem);
   if (e != cudaSuccess) return e;
-  if ((e = registers_do<kLoss>()) != cudaSuccess || (e = registers_do<kSoftmax>()) != cudaSuccess) return e;
+  if ((e = registers_do<kLoss>()) != cudaSuccess || (e = registers_do<kSoftmax>()) != cudaSuccess ||
+      (e = registers_do<kGrad>()) != cudaSuccess)
+    return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
   cfg.blockDim = dim3(kThreads);
@@ -971,6 +1002,9 @@ cudaError_t launch_ce_gradient(const CeCall &c, cudaStream_t s) {
       !panel_map(&g.a[1], c.loss->at.G, c.rows, p.piece, 64) || !panel_map(&g.b[1], c.loss->at.x, c.rows, c.d, 64))
     return cudaErrorInvalidValue;
   const int64_t nm = c.rows / kCeTile, nd = tiles_of(c.d);
+  // Whether any sum is longer than a segment: of tokens, or of a split of a piece.
+  const int64_t steps = std::max(g.want_dw ? c.rows : 0, g.want_dx ? (p.piece + c.splits - 1) / c.splits : 0) / kCeStep;
+  const bool parts = steps >= kGradSegment;
   for (int64_t first = 0; first < tiles; first += per) {
     p.first_tile = g.first_tile = first;
     p.tiles = g.tiles = (int)std::min(per, tiles - first);
@@ -980,7 +1014,8 @@ cudaError_t launch_ce_gradient(const CeCall &c, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     g.add_dx = first > 0;
     const int64_t units = (g.want_dx ? nm * nd * g.splits : 0) + (g.want_dw ? g.tiles * nd : 0);
-    if ((e = launch<kGrad, false>(g, units, c.loss->clusters, s)) != cudaSuccess) return e;
+    e = parts ? launch<kGrad, true>(g, units, c.loss->clusters, s) : launch<kGrad, false>(g, units, c.loss->clusters, s);
+    if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }

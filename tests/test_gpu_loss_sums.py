@@ -1,9 +1,10 @@
 """Sums of the dense head's loss and its gradient, where their rounding shows.
 
 Tensor cores add to a running sum and cut what does not fit into fp32: by less than a unit in the last place, 2^-23 of
-the sum so far, for every 16 products, and always toward zero.  A logit is cut into parts of 1024 products for that, which
-are added to one another by ordinary additions, each within 2^-24: it is within 64 * 2^-23 of its absolute terms beside
-these.  The gradients' own sums are of 2000 products at most here.  The gradient computes a logit as the loss does, in the same parts: what it is off by is the same
+the sum so far, for every 16 products, and always toward zero.  A sum is cut into parts for that (of 1024 products for
+a logit, of 8192 for an element of a gradient) and the parts are added to one another by ordinary additions, each within
+2^-24.  So a logit is within 64 * 2^-23 of its absolute terms beside its additions, a gradient's element within
+512 * 2^-23 of them.  The gradient computes a logit as the loss does, in the same parts: what it is off by is the same
 in l and in lse, and exp(l - lse) does not see what both have.
 """
 
@@ -74,3 +75,67 @@ def test_tokens_that_the_model_is_sure_of(M, d, ldx, dtype):
     # The whole row of a token, held against its own size: 1e-4 of the target's p would be all of it for the surest.
     rows = (dx.double() - G @ ww).norm(dim=1) / (G @ ww).norm(dim=1)
     assert (rows <= 2 * delta + 2.0 ** -15 + 2 * HALF_STEP[dtype] + 2.0 ** -16 / sure[:, 0]).all()
+
+
+def _mean_off(got, want):
+    """The mean of the errors relative to the values, with their signs: roundings to nearest cancel in it."""
+    return ((got.double() - want) / want).mean().item()
+
+
+@pytest.mark.parametrize("M,wide", [(1 << 18, 64), (40000, 300)], ids=str)
+def test_sums_over_many_tokens_are_not_cut_short(M, wide):
+    """Terms of one sign.  Logits are 0 and factors powers of two: p is 1 / V and G exact.  fp16's rounding of an element
+    of dw is 2^-11 at most and 2^-12.5 in the mean square or less, either way: of 60 * 64 elements 2^-18 in the mean, and
+    four times that at most."""
+    torch = _torch()
+    V = 64
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    x = (0.5 + torch.rand((M, wide), generator=gen, device="cuda")).half()
+    w = torch.zeros((V, (wide + 7) // 8 * 8), dtype=torch.float16, device="cuda")[:, :wide]
+    t = torch.full((M,), V - 1, dtype=torch.int32, device="cuda")
+    g = torch.full((M,), 2.0 ** -10, device="cuda")
+    dw = _run(x, w, t, g)[3]
+    want = (x.double().sum(dim=0) * 2.0 ** -16).expand(V - 1, wide)
+    assert abs(_mean_off(dw[:V - 1], want)) <= CHAIN + (M / 8192 + 1) * U + 2.0 ** -16
+    assert abs(_mean_off(dw[V - 1:], -want[:1] * (V - 1))) <= CHAIN + (M / 8192 + 1) * U + 2.0 ** -13.5
+
+
+@pytest.mark.parametrize("M,V", [(40, 1 << 18), (200, 1 << 18), (2500, 1 << 17)], ids=str)
+def test_sums_over_a_large_vocabulary_are_not_cut_short(M, V):
+    """The same for dx: the targets' row of w is 0, the others are positive.  Of 8192 columns, the same for every token,
+    roundings are 2^-19 in the mean, and four times that at most; p, a power of two but for 2^-20 of itself, may be
+    rounded to one in G."""
+    torch = _torch()
+    d = 8192
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    w = torch.empty((V, d), dtype=torch.float16, device="cuda")
+    for part in w.split(1 << 14):
+        part.copy_(0.5 + torch.rand(part.shape, generator=gen, device="cuda"))
+    w[5] = 0
+    x = torch.zeros((M, d), dtype=torch.float16, device="cuda")
+    t = torch.full((M,), 5, dtype=torch.int32, device="cuda")
+    dx = _run(x, w, t, torch.ones(M, device="cuda"))[2]
+    want = sum(part.double().sum(dim=0) for part in w.split(1 << 14)) / V
+    assert (dx == dx[0]).all()
+    assert abs(_mean_off(dx[0], want)) <= CHAIN + (V / 8192 + 32) * U + 2.0 ** -17 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("M,V,d", [(1 << 20, 40, 8), (2, 1 << 24, 8), (3, 300, 1 << 16)], ids=str)
+def test_largest_sizes_within_their_chains(M, V, d):
+    """Bounds that go by how long a sum on the tensor cores is.  Targets of the vocabulary's first half, states and factors
+    of one sign: gradients are large beside the bounds."""
+    torch = _torch()
+    x, w, t, g = _draw(M, V, d, "bf16", seed=43)
+    x, t, g = x.abs(), t % (V // 2), g.abs()
+    _, _, dx, dw = _run(x, w, t, g)
+    x, w, g = x.double(), w.double(), g.double()
+    at = t.long()[:, None]
+    G = torch.softmax(x @ w.t(), dim=1)
+    off = (2.0 ** -15 + 2 * V / 4096 * U) * G + 2.0 ** -126
+    G.scatter_add_(1, at, torch.full((M, 1), -1.0, dtype=torch.float64, device="cuda"))
+    off = (off + HALF_STEP["bf16"] * G.abs()) * g.abs()[:, None]
+    G *= g[:, None]
+    for got, exact, bound in ((dx, G @ w, (off + (CHAIN + (V / 8192 + 32) * U) * G.abs()) @ w.abs()),
+                              (dw, G.t() @ x, (off + (CHAIN + (M / 8192 + 32) * U) * G.abs()).t() @ x.abs())):
+        _near(got, exact, bound + HALF_STEP["bf16"] * (exact.abs() + bound) + 2.0 ** -126, "gradient")
+        assert exact.norm() > 4 * bound.norm() or V == 1 << 24 and got is dw
