@@ -23,14 +23,15 @@ namespace {
 
 // A sum as two floats: hi, and lo that takes what rounding hi lost (D. Knuth, The Art
 // of Computer Programming 2, 4.2.2: the error of a sum is a float, and found by
-// six additions).  The intrinsics are never joined to fused operations.
+// six additions).  The intrinsics are never joined to fused operations.  The two low parts are added first: so two lanes that
+// add each other's sums get the same (hi's error is exact in either order), and all lanes of a row one factor.
 struct Sum2 {
   float hi = 0.f, lo = 0.f;
   __device__ __forceinline__ void add(float v, float rest) {
     const float s = __fadd_rn(hi, v), b = __fsub_rn(s, hi);
     const float e = __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(v, b));
     hi = s;
-    lo = __fadd_rn(lo, __fadd_rn(e, rest));
+    lo = __fadd_rn(e, __fadd_rn(lo, rest));
   }
 };
 
