@@ -628,7 +628,8 @@ ARCHEAD_API archead_status archead_rms_norm_backward(archead_norm *norm, const a
  *                     ce[m]  = lse[m] - l[m][targets[m]]          (nats)
  *   ce fp32 [M]; lse fp32 [M], or NULL where no gradient follows.  A token whose
  *   target is ignore_index has ce and lse 0.  Any other target outside [0, V)
- *   gives NaN for both and latches ARCHEAD_ERR_TARGET_RANGE.
+ *   gives NaN for both and latches ARCHEAD_ERR_TARGET_RANGE.  A logit of +infinity makes lse infinite (and ce,
+ *   but NaN where it is the target's own), and the token's gradients NaN: exp(inf - inf).
  * archead_linear_ce_backward: of the gradient grad_ce (fp32 [M]) of ce, with
  *     G[m][n] = grad_ce[m] (exp(l[m][n] - lse[m]) - [n == targets[m]]),
  *     dx = G w,   dw = G^T x  (+ dw: accumulate 1),

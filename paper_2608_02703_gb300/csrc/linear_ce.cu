@@ -335,7 +335,7 @@ __device__ __forceinline__ void sum_columns(float (&v)[32], int64_t base, int64_
     m = top;
   }
   // (Differences first: of large logits a product with log2 e would be rounded by more than the difference is.)
-  const float minus = m == -INFINITY ? 0.f : -m;  // (nothing but -inf so far)
+  const float minus = fabsf(m) == INFINITY ? 0.f : -m;  // (nothing but -inf so far, or a sum that is infinite)
   float2 part[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {

@@ -145,6 +145,7 @@ __device__ __forceinline__ LsePair joined(LsePair a, LsePair b) {
   if (a.m == -INFINITY) return {b.m, a.s + b.s};  // (s is 0, or NaN)
   if (b.m == -INFINITY) return {a.m, a.s + b.s};
   const float m = fmaxf(a.m, b.m);
+  if (m == INFINITY) return {m, a.s + b.s};  // (s is infinite there)
   return {m, a.s * expf(a.m - m) + b.s * expf(b.m - m)};
 }
 
