@@ -635,9 +635,10 @@ ARCHEAD_API archead_status archead_rms_norm_backward(archead_norm *norm, const a
  *     dx = G w,   dw = G^T x  (+ dw: accumulate 1),
  *   from the lse of the forward with the same arguments.  dx [M][d] and dw [V][d]
  *   are of x's type, each rounded once from fp32 sums; one of them may be NULL (a
- *   frozen head, or frozen states).  G is rounded to 16 bits on its way into the
- *   products, in fp16 times a power of two by the largest |grad_ce|: an error of half
- *   a step of the type in each of its elements.  Logits are computed again, in pieces of the
+ *   frozen head, or frozen states).  Up to 64 tokens G goes into the products in two parts of 16 bits (an error of
+ *   half a step of half a step of the type in each of its elements), with more rounded to 16 bits (half a step, which
+ *   leaves dx and dw at some 1.4 times what their own rounding does); in fp16 times a power of two by the largest
+ *   |grad_ce|, so that no less than 2^-39 of that is lost.  Logits are computed again, in pieces of the
  *   vocabulary.  Tokens that are ignored, or whose grad_ce is 0, have dx 0 and take
  *   no part (whatever their rows of x hold); a token whose target was out of range
  *   makes its row of dx and all of dw NaN.

@@ -85,6 +85,7 @@ struct Params {
   int a_rows;              // token rows of a block's part of A that are loaded: 32, 64 or 128
   int a_both;              // the second block has tokens, too
   int direct, M;           // x is read where it lies, and all M tokens have rows (kLoss, kSoftmax)
+  int half;                // rows of G's first part, where it has a second one behind it (kSoftmax: kTwo), else 0
   int splits, dx_pitch, add_dx, want_dx, want_dw, box_out;
   void *dw;
   int64_t lddw;
@@ -181,7 +182,7 @@ struct Units {
       return;
     }
     ks = (int)((cols + kCeStep - 1) / kCeStep);
-    kt = (count + kCeStep - 1) / kCeStep;
+    kt = p.half == 0 ? (count + kCeStep - 1) / kCeStep : count == 0 ? 0 : 2 * p.half / kCeStep;
     nd = (int)((p.d + kCeTile - 1) / kCeTile);
     const int n_dx = p.want_dx ? nm * nd * p.splits : 0, n_dw = p.want_dw ? p.tiles * nd : 0;
     // (A unit of dW takes its epilogue's time, some six steps, at least.)
@@ -286,17 +287,17 @@ struct OutBox {
     if (kBoxes > 1) turn ^= 1;
   }
   // Columns 8 j .. 8 j + 7 of this lane's row.
-  __device__ __forceinline__ void put(int j, uint32_t a, uint32_t b, uint32_t c, uint32_t d) const {
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(a),
+  __device__ __forceinline__ void put(int j, uint32_t a, uint32_t b, uint32_t c, uint32_t d, int off = 0) const {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + off + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(a),
                  "r"(b), "r"(c), "r"(d)
                  : "memory");
   }
-  __device__ __forceinline__ void store(const CUtensorMap *map, int col, int row) const {
+  __device__ __forceinline__ void store(const CUtensorMap *map, int col, int row, int off = 0) const {
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
       asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map), "r"(col),
-                   "r"(row), "r"(at)
+                   "r"(row), "r"(at + off)
                    : "memory");
       asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
     }
@@ -359,8 +360,19 @@ __device__ __forceinline__ void add_columns(uint32_t taddr, float (&held)[32]) {
   for (int j = 0; j < 32; ++j) held[j] += v[j];
 }
 
-// kParts: sums over more than a segment are taken in parts.
-template <Mode kMode, bool kParts>
+// What rounding to w, 16 bits each, took from a and b, as 16 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t rest16(float a, float b, uint32_t w) {
+  float2 r;
+  if constexpr (__is_same(T, __nv_bfloat16))
+    r = make_float2(bf16_lo(w), bf16_hi(w));
+  else
+    r = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+  return pack16<T>(a - r.x, b - r.y);
+}
+
+// kParts: sums over more than a segment are taken in parts.  kTwo: G has two parts (kSoftmax).
+template <Mode kMode, bool kParts, bool kTwo = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     linear_ce_kernel(const __grid_constant__ Params p) {
   using G = Geom<kMode>;
@@ -483,7 +495,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             kinds[r.s] = u.dw;
             if (n >= early) {
               if (leader) mbar_arrive_expect_tx(&full[r.s], stage_bytes(u.dw));
-              load_b(r.s, u.dw, b_row, k * kCeStep);
+              load_b(r.s, u.dw, b_row, kMode == kGrad && u.dw && p.half > 0 ? 0 : k * kCeStep);  // (x is the same for both parts)
             }
             load_a(r.s, u.dw, a_row, k * kCeStep);
           }
@@ -558,7 +570,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const float unscale = kMode == kGrad ? p.at.header->unscale : 1.f;
     while (units.next(p, u)) {
       const int64_t row = (int64_t)u.row * kCeTile + 128 * (int)rank + 32 * quad + lane;
-      bool live = row < count;
+      // (Of a G in two parts the second's products with W have rows of their own, which are added with the splits of dx.)
+      const auto counts = [&](int64_t at) {
+        return kMode == kGrad && p.half > 0 ? at < 2 * p.half && (at & (p.half - 1)) < count : at < count;
+      };
+      bool live = counts(row);
       // (under way while the MMAs are waited for)
       const int t = kMode != kGrad && live ? p.at.target[row] : -1;
       const float lse = kMode == kSoftmax && live ? p.at.lse[row] : 0.f;
@@ -572,8 +588,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // for l = 20 of 4096 products in one sum).
       // (G's rows up to a whole stage are read as dW's summed dimension; rows past the tokens that count are zeros
       // there, and of no account in dx.)
-      const int needed = kMode == kSoftmax ? (count + kCeStep - 1) / kCeStep * kCeStep : count;
-      const bool wanted = kMode == kGrad && u.dw ? p.first_tile * kCeTile + row0 < p.V : row0 < needed;
+      const int stage_rows = kTwo ? p.half : (count + kCeStep - 1) / kCeStep * kCeStep;
+      const bool wanted = kMode == kSoftmax ? row0 < stage_rows
+                          : kMode == kGrad && u.dw ? p.first_tile * kCeTile + row0 < p.V : counts(row0);
       const int chunks = kMode == kGrad ? kCeTile / 32 : p.nt / 32;
       // The sum of all parts but the last.
       const auto add_parts = [&](float (&held)[4][32]) {
@@ -664,11 +681,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               for (int j = 0; j < 32; ++j) v[j] = j < lim ? v[j] : 0.f;
             }
             if ((c & 1) == 0) box.begin();
+            // (The second part goes through the box of a warp that has no tokens: those of two quarters on.)
+            constexpr int kSecondBox = 2 * kBoxBytes;
+            const auto put = [&](auto type) {
+              using T = decltype(type);
 #pragma unroll
-            for (int j = 0; j < 32; j += 8)
-              box.put((c & 1) * 4 + j / 8, pack_out(v[j], v[j + 1], p.fp16), pack_out(v[j + 2], v[j + 3], p.fp16),
-                      pack_out(v[j + 4], v[j + 5], p.fp16), pack_out(v[j + 6], v[j + 7], p.fp16));
-            if (c & 1) box.store(&p.out, 0, (u.col * p.nt + 32 * c) / 64 * (int)p.rows + (int)row0);
+              for (int j = 0; j < 32; j += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = pack16<T>(v[j + 2 * i], v[j + 2 * i + 1]);
+                box.put((c & 1) * 4 + j / 8, w[0], w[1], w[2], w[3]);
+                if constexpr (kTwo) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) w[i] = rest16<T>(v[j + 2 * i], v[j + 2 * i + 1], w[i]);
+                  box.put((c & 1) * 4 + j / 8, w[0], w[1], w[2], w[3], kSecondBox);
+                }
+              }
+            };
+            if (p.fp16) put(__half{});
+            else put(__nv_bfloat16{});
+            if (c & 1) {
+              const int to = (u.col * p.nt + 32 * c) / 64 * (int)p.rows + (int)row0;
+              box.store(&p.out, 0, to);
+              if constexpr (kTwo) box.store(&p.out, 0, to + p.half, kSecondBox);
+            }
           };
           if constexpr (kParts) {
 #pragma unroll
@@ -849,15 +885,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-template <Mode kMode, bool kParts>
+template <Mode kMode, bool kParts, bool kTwo = false>
 cudaError_t launch(const Params &p, int64_t units, int clusters, cudaStream_t s) {
-  auto kern = linear_ce_kernel<kMode, kParts>;
-  cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), Geom<kMode>::kSmem);
+  auto kern = linear_ce_kernel<kMode, kParts, kTwo>;
+  constexpr int kSmem = Geom<kMode>::kSmem;
+  cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * std::max<int64_t>(1, std::min<int64_t>(units, clusters))));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Geom<kMode>::kSmem;
+  cfg.dynamicSmemBytes = kSmem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -924,10 +961,10 @@ int64_t logits_units(const CeCall &c, const Params &p) {
 }  // namespace
 
 // (A block that was launched with fewer registers than it hands on would wait for them.)
-template <Mode kMode>
+template <Mode kMode, bool kTwo = false>
 static cudaError_t registers_do() {
   cudaFuncAttributes a;
-  const cudaError_t e = cudaFuncGetAttributes(&a, linear_ce_kernel<kMode, true>);
+  const cudaError_t e = cudaFuncGetAttributes(&a, linear_ce_kernel<kMode, true, kTwo>);
   return e != cudaSuccess ? e : a.numRegs * kThreads < Geom<kMode>::kRegsInAll ? cudaErrorInvalidConfiguration : cudaSuccess;
 }
 
@@ -937,7 +974,7 @@ cudaError_t ce_clusters(int *clusters) {
   cudaError_t e = opt_in_smem(reinterpret_cast<const void *>(kern), kSmem);
   if (e != cudaSuccess) return e;
   if ((e = registers_do<kLoss>()) != cudaSuccess || (e = registers_do<kSoftmax>()) != cudaSuccess ||
-      (e = registers_do<kGrad>()) != cudaSuccess)
+      (e = registers_do<kSoftmax, true>()) != cudaSuccess || (e = registers_do<kGrad>()) != cudaSuccess)
     return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
@@ -992,6 +1029,8 @@ cudaError_t launch_ce_gradient(const CeCall &c, cudaStream_t s) {
   p.lddw = c.lddw;
   p.accumulate = c.accumulate;
   Params g = p;  // of the products with G
+  p.half = g.half = c.half;
+  if (c.half > 0) g.a_rows = 2 * c.half;
   if (g.want_dx && !make_tma_map_f32(&g.out_dx, c.loss->at.dx, c.rows * c.splits, c.dx_pitch, 32)) return cudaErrorInvalidValue;
   // (A box is cut off at whole 16 bytes past the matrix's edge: what lies between rows would be written.)
   g.box_out = g.want_dw && !c.accumulate && c.d % 8 == 0;
@@ -1005,12 +1044,13 @@ cudaError_t launch_ce_gradient(const CeCall &c, cudaStream_t s) {
   // Whether any sum is longer than a segment: of tokens, or of a split of a piece.
   const int64_t steps = std::max(g.want_dw ? c.rows : 0, g.want_dx ? (p.piece + c.splits - 1) / c.splits : 0) / kCeStep;
   const bool parts = steps >= kGradSegment;
+  const bool cut = c.d > kSegment * kCeStep;  // (the logits' sums)
+  const auto of_g = c.half > 0 ? cut ? launch<kSoftmax, true, true> : launch<kSoftmax, false, true>
+                          : cut ? launch<kSoftmax, true> : launch<kSoftmax, false>;
   for (int64_t first = 0; first < tiles; first += per) {
     p.first_tile = g.first_tile = first;
     p.tiles = g.tiles = (int)std::min(per, tiles - first);
-    const int64_t of_g = logits_units(c, p);
-    cudaError_t e = c.d > kSegment * kCeStep ? launch<kSoftmax, true>(p, of_g, c.loss->clusters, s)
-                                             : launch<kSoftmax, false>(p, of_g, c.loss->clusters, s);
+    cudaError_t e = of_g(p, logits_units(c, p), c.loss->clusters, s);
     if (e != cudaSuccess) return e;
     g.add_dx = first > 0;
     const int64_t units = (g.want_dx ? nm * nd * g.splits : 0) + (g.want_dw ? g.tiles * nd : 0);

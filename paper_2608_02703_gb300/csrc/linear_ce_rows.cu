@@ -55,9 +55,14 @@ __global__ void __launch_bounds__(kThreads) ce_gather_kernel(const __grid_consta
       }
     }
   };
-  const auto clear = [&](int64_t row, int k) {
-    *reinterpret_cast<uint4 *>(p.at.x + ((int64_t)(k >> 6) * p.rows + row) * 64 + (k & 63)) = make_uint4(0, 0, 0, 0);
+  // Column k of a row: panel k / 64.
+  const auto place_of = [&](int64_t row, int k) { return p.at.x + ((int64_t)(k >> 6) * p.rows + row) * 64 + (k & 63); };
+  const bool twice = p.half == kCeStep / 2;  // (G's two parts are one stage, and x stands behind itself)
+  const auto put8 = [&](int64_t row, int k, uint4 v) {
+    *reinterpret_cast<uint4 *>(place_of(row, k)) = v;
+    if (twice) *reinterpret_cast<uint4 *>(place_of(row + p.half, k)) = v;
   };
+  const auto clear = [&](int64_t row, int k) { put8(row, k, make_uint4(0, 0, 0, 0)); };
   if (!p.direct || gradient) load(m0 + warp, 0);
   int2 n = make_int2(0, 0);  // before m0, in all
   float most = 0.f;
@@ -102,15 +107,17 @@ __global__ void __launch_bounds__(kThreads) ce_gather_kernel(const __grid_consta
     if (p.direct && m < m1 && !in) {
       for (int k = 8 * lane; k < p.x_pitch; k += 256) clear(m, k);
     } else if (m < m1 && in) {
-      // Column k of the row: panel k / 64.
-      const auto to = [&](int k) { return p.at.x + ((int64_t)(k >> 6) * p.rows + place) * 64 + (k & 63); };
+      const auto put = [&](int k, uint16_t v) {
+        *place_of(place, k) = v;
+        if (twice) *place_of(place + p.half, k) = v;
+      };
       if (vec) {
         for (int k0 = 0; k0 < p.d; k0 += 256 * kCopyLoads) {
           if (k0 > 0) load(m, k0);
 #pragma unroll
           for (int i = 0; i < kCopyLoads; ++i) {
             const int k = k0 + 8 * (lane + 32 * i);
-            if (k < p.d) *reinterpret_cast<uint4 *>(to(k)) = held[i];
+            if (k < p.d) put8(place, k, held[i]);
           }
         }
       } else {
@@ -122,15 +129,15 @@ __global__ void __launch_bounds__(kThreads) ce_gather_kernel(const __grid_consta
             if (k + 32 * i < p.d) v[i] = from[k + 32 * i];
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (k + 32 * i < p.d) *to(k + 32 * i) = v[i];
+            if (k + 32 * i < p.d) put(k + 32 * i, v[i]);
         }
       }
-      for (int k = p.d + lane; k < p.x_pitch; k += 32) *to(k) = 0;
+      for (int k = p.d + lane; k < p.x_pitch; k += 32) put(k, 0);
     }
     load(m + kThreads / 32, 0);
   }
   if (blockIdx.x == gridDim.x - 1) {
-    const int end = (rows + kCeStep - 1) / kCeStep * kCeStep;
+    const int end = twice ? p.half : (rows + kCeStep - 1) / kCeStep * kCeStep;
     for (int r = rows + warp; r < end; r += kThreads / 32)
       for (int k = 8 * lane; k < p.x_pitch; k += 256) clear(r, k);
   }
@@ -196,8 +203,8 @@ __global__ void __launch_bounds__(kFinishTokens *kFinishLanes) ce_finish_kernel(
   if (p.lse) p.lse[m] = lse;
 }
 
-// dx's rows: the sum of the splits, in order, without the factors' scale; zeros for tokens that do not
-// count.  A thread takes four columns.
+// dx's rows: the sum of the splits, in order (and of G's second part, in rows of its own), without the
+// factors' scale; zeros for tokens that do not count.  A thread takes four columns.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) ce_dx_kernel(const CeDxParams p) {
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
@@ -209,12 +216,16 @@ __global__ void __launch_bounds__(kThreads) ce_dx_kernel(const CeDxParams p) {
   float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
   if (place >= 0) {
     const float *from = p.at.dx + (int64_t)place * p.pitch + k;  // (columns past d are there, to a whole tile)
-    const int64_t step = p.rows * p.pitch;
-    for (int i = 0; i < p.splits; i += 8) {
+    const int64_t step = p.rows * p.pitch, half = (int64_t)p.half * p.pitch;
+    const int parts = p.half > 0 ? 2 * p.splits : p.splits;
+    for (int i = 0; i < parts; i += 8) {
       float4 v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[j] = i + j < p.splits ? *reinterpret_cast<const float4 *>(from + (i + j) * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int j = 0; j < 8; ++j) {
+        const int at = i + j;
+        v[j] = at < parts ? *reinterpret_cast<const float4 *>(from + (p.half > 0 ? (at >> 1) * step + (at & 1) * half : at * step))
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) t.x += v[j].x, t.y += v[j].y, t.z += v[j].z, t.w += v[j].w;
     }

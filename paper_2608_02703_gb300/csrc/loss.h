@@ -68,6 +68,7 @@ struct CeRowsParams {
   int32_t ignore;
   int64_t M, ldx, V, rows;
   int d, x_pitch, rows_per_block;
+  int half;          // the gradient's copy of x stands there again from row 32 on, where it is 32 (see ce_half)
   bool direct;       // one tile of tokens, whose logits are computed from x as it lies: every token keeps its row
   CeScratch at;
 };
@@ -101,6 +102,7 @@ struct CeDxParams {
   void *dx;
   int64_t M, ld, rows;
   int d, pitch, splits;
+  int half;  // see CeCall
   bool fp16, vec;
   CeScratch at;
 };
@@ -120,8 +122,15 @@ struct CeCall {
   int64_t lddw;
   int accumulate;
   bool want_dx;
+  int half;      // rows of G's first part, where it has two (see ce_half), else 0
   int splits, dx_pitch;
 };
+// Up to 64 tokens G is held in two parts of 16 bits, the value and what its rounding took, which is as good as 32 bits:
+// the second has the rows behind the first, which a block's half of A has room for, so that the products with W are the
+// same and dW takes one more step of 64 rows (up to 32 tokens none).  4 tokens x 4096 x 512, loss and gradients 26.9 ->
+// 27.7 us, 64 x 262144 x 2560 900 -> 935; with G in 16 bits dx and dW stood at 1.4 times what their own rounding leaves.
+// More tokens would take twice the MMAs, which bound those calls: there G is rounded to 16 bits.
+inline int ce_half(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 0; }
 int64_t ce_piece_tiles(const archead_loss *l, const CeCall &c);  // tiles of a piece
 int ce_dx_splits(const archead_loss *l, int64_t M, int64_t V, int64_t d, bool want_dw);
 cudaError_t ce_clusters(int *clusters);  // pairs of blocks that the current device runs at once

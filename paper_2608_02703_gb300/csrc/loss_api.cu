@@ -111,6 +111,7 @@ CeRowsParams gathering(const archead_loss *l, const Call &c, int32_t ignore, con
   p.x_pitch = (int)up(c.d, kCeStep);
   p.rows = up(c.M, kCeTile);
   p.direct = reads_directly(c);
+  p.half = grad ? ce_half(c.M) : 0;
   p.at = l->at;
   return p;
 }
@@ -238,6 +239,7 @@ archead_status archead_linear_ce_backward(archead_loss *loss, const void *x, con
   p.lddw = lddw;
   p.accumulate = accumulate;
   p.want_dx = dx != nullptr;
+  p.half = ce_half(M);
   p.splits = ce_dx_splits(loss, M, V, d, dw != nullptr);
   p.dx_pitch = (int)up(d, kCeTile);
   AH_TRY(launch_ce_gradient(p, s));
@@ -251,6 +253,7 @@ archead_status archead_linear_ce_backward(archead_loss *loss, const void *x, con
     f.pitch = p.dx_pitch;
     f.splits = p.splits;
     f.fp16 = p.fp16;
+    f.half = p.half;
     f.at = loss->at;
     AH_TRY(launch_ce_dx(f, s));
   }

@@ -139,3 +139,35 @@ def test_largest_sizes_within_their_chains(M, V, d):
                               (dw, G.t() @ x, (off + (CHAIN + (M / 8192 + 32) * U) * G.abs()).t() @ x.abs())):
         _near(got, exact, bound + HALF_STEP["bf16"] * (exact.abs() + bound) + 2.0 ** -126, "gradient")
         assert exact.norm() > 4 * bound.norm() or V == 1 << 24 and got is dw
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("M,V,d,ignored", [(1, 3000, 512, 0), (4, 4096, 512, 0), (33, 3001, 200, 0.3), (64, 3000, 1500, 0),
+                                           (32, 2000, 77, 0.1), (50, 600000, 64, 0)], ids=str)
+def test_gradients_of_few_tokens_are_rounded_once(M, V, d, ignored, dtype):
+    """Up to 64 tokens G is held in two parts: of an element half a step of half a step is lost, in fp16 no less than half of
+    2^-24 of its scale.  So what dx and dw are off by is, but for these errors, the rounding of their values: a distance
+    to the nearest number of the type changes by no more than the value does."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(V + d)
+    x = torch.randn((M, d), generator=gen, device="cuda").to(_dtype(dtype))
+    w = torch.empty((V, (d + 7) // 8 * 8), dtype=_dtype(dtype), device="cuda")[:, :d]
+    w.copy_(torch.randn((V, d), generator=gen, device="cuda") * (2.5 / d ** 0.5))
+    t = torch.randint(0, V, (M,), generator=gen, device="cuda").to(torch.int32)
+    t[torch.rand(M, generator=gen, device="cuda") < ignored] = IGNORED
+    g = 0.5 + torch.rand(M, generator=gen, device="cuda")
+    _, _, dx, dw = _run(x, w, t, g)
+    live = (t != IGNORED).double()[:, None]
+    xx, ww, gg, at = x.double(), w.double(), g.double()[:, None] * live, t.clamp_min(0).long()[:, None]
+    logits = xx @ ww.t()
+    delta = (LOGIT + 16 * U) * (xx.abs() @ ww.abs().t()).max()
+    G = torch.softmax(logits, dim=1)
+    off = (2 * delta + 2.0 ** -15) * G + 2.0 ** -126
+    G.scatter_add_(1, at, torch.full((M, 1), -1.0, dtype=torch.float64, device="cuda"))
+    G, off = G * gg, (off + HALF_STEP[dtype] ** 2 * G.abs()) * gg
+    if dtype == "fp16":
+        off += 2.0 ** -25 * 2.0 ** -14 * gg.max()
+    chain = min(CHAIN, V / 16 * 2.0 ** -23)
+    for got, exact, bound in ((dx, G @ ww, (off + chain * G.abs()) @ ww.abs()), (dw, G.t() @ xx, (off + CHAIN / 64 * G.abs()).t() @ xx.abs())):
+        rounding = (exact.to(got.dtype).double() - exact).norm()
+        assert (got.double() - exact).norm() <= rounding + 2 * (bound + TINY[dtype]).norm()
