@@ -644,7 +644,7 @@ ARCHEAD_API archead_status archead_rms_norm_backward(archead_norm *norm, const a
  *   makes its row of dx and all of dw NaN.
  *   dx may be x with the same row distance.  M == 0 leaves dw 0 (accumulate: as it was).
  *   Tensor cores round their sums toward zero: within 2^-17 of its absolute terms for a logit, which is cut into
- *   sums of 1024 products, alike in both entries, and within 2^-14 for dx and dw, of 8192.
+ *   sums of 1024 products, alike in both entries, and within 2^-13 for dx and dw, of 16384.
  * Rows are ldx, ldw, lddx, lddw elements apart (>= d).  The rows of w and dw start on
  *   16 bytes (ldw and lddw multiples of 8; else ARCHEAD_ERR_UNSUPPORTED), all else
  *   is aligned to its elements.  Any V, M and d.  Results do not depend on what the

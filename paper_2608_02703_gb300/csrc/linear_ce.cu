@@ -49,9 +49,9 @@ constexpr int kEpiWarps = 8;
 constexpr int kThreads = 128 + 32 * kEpiWarps;
 // Steps of a sum in tensor memory where it is taken in parts, which epilogue warps add in registers: of a logit, and of
 // an element of dx or dW.  Tensor cores round their additions toward zero, by up to 2^-23 of the sum so far each, and
-// always so.  For a logit see the epilogue; of a gradient's terms of one sign 8192 lose some 2^-15 in this way (in one
+// always so.  For a logit see the epilogue; of a gradient's terms of one sign 16384 lose some 2^-14 in this way (in one
 // sum 2^18 lost 1.2e-3, more than fp16's rounding).
-constexpr int kSegment = 16, kGradSegment = 128;
+constexpr int kSegment = 16, kGradSegment = 256;
 constexpr int kBoxBytes = 32 * 64 * 2;               // outputs that a warp stages: 32 rows of 64 columns
 // The gradient's outputs of few tokens are bound by what leaves: there a warp fills a box while its last one is read.
 // The loss has no boxes, and epilogue warps that hold a unit's sums in registers.

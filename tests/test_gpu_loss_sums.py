@@ -2,9 +2,9 @@
 
 Tensor cores add to a running sum and cut what does not fit into fp32: by less than a unit in the last place, 2^-23 of
 the sum so far, for every 16 products, and always toward zero.  A sum is cut into parts for that (of 1024 products for
-a logit, of 8192 for an element of a gradient) and the parts are added to one another by ordinary additions, each within
+a logit, of 16384 for an element of a gradient) and the parts are added to one another by ordinary additions, each within
 2^-24.  So a logit is within 64 * 2^-23 of its absolute terms beside its additions, a gradient's element within
-512 * 2^-23 of them.  The gradient computes a logit as the loss does, in the same parts: what it is off by is the same
+1024 * 2^-23 of them.  The gradient computes a logit as the loss does, in the same parts: what it is off by is the same
 in l and in lse, and exp(l - lse) does not see what both have.
 """
 
@@ -17,7 +17,7 @@ from .test_gpu_loss import HALF_STEP, IGNORED, U, _build, _draw, _dtype, _near, 
 pytestmark = pytest.mark.gpu
 
 LOGIT = 64 * 2.0 ** -23
-CHAIN = 512 * 2.0 ** -23
+CHAIN = 1024 * 2.0 ** -23
 TINY = {"bf16": 2.0 ** -126, "fp16": 2.0 ** -25}
 
 
@@ -96,8 +96,8 @@ def test_sums_over_many_tokens_are_not_cut_short(M, wide):
     g = torch.full((M,), 2.0 ** -10, device="cuda")
     dw = _run(x, w, t, g)[3]
     want = (x.double().sum(dim=0) * 2.0 ** -16).expand(V - 1, wide)
-    assert abs(_mean_off(dw[:V - 1], want)) <= CHAIN + (M / 8192 + 1) * U + 2.0 ** -16
-    assert abs(_mean_off(dw[V - 1:], -want[:1] * (V - 1))) <= CHAIN + (M / 8192 + 1) * U + 2.0 ** -13.5
+    assert abs(_mean_off(dw[:V - 1], want)) <= CHAIN + (M / 16384 + 1) * U + 2.0 ** -16
+    assert abs(_mean_off(dw[V - 1:], -want[:1] * (V - 1))) <= CHAIN + (M / 16384 + 1) * U + 2.0 ** -13.5
 
 
 @pytest.mark.parametrize("M,V", [(40, 1 << 18), (200, 1 << 18), (2500, 1 << 17)], ids=str)
@@ -117,7 +117,7 @@ def test_sums_over_a_large_vocabulary_are_not_cut_short(M, V):
     dx = _run(x, w, t, torch.ones(M, device="cuda"))[2]
     want = sum(part.double().sum(dim=0) for part in w.split(1 << 14)) / V
     assert (dx == dx[0]).all()
-    assert abs(_mean_off(dx[0], want)) <= CHAIN + (V / 8192 + 32) * U + 2.0 ** -17 + 2.0 ** -20
+    assert abs(_mean_off(dx[0], want)) <= CHAIN + (V / 16384 + 32) * U + 2.0 ** -17 + 2.0 ** -20
 
 
 @pytest.mark.parametrize("M,V,d", [(1 << 20, 40, 8), (2, 1 << 24, 8), (3, 300, 1 << 16)], ids=str)
@@ -135,8 +135,8 @@ def test_largest_sizes_within_their_chains(M, V, d):
     G.scatter_add_(1, at, torch.full((M, 1), -1.0, dtype=torch.float64, device="cuda"))
     off = (off + HALF_STEP["bf16"] * G.abs()) * g.abs()[:, None]
     G *= g[:, None]
-    for got, exact, bound in ((dx, G @ w, (off + (CHAIN + (V / 8192 + 32) * U) * G.abs()) @ w.abs()),
-                              (dw, G.t() @ x, (off + (CHAIN + (M / 8192 + 32) * U) * G.abs()).t() @ x.abs())):
+    for got, exact, bound in ((dx, G @ w, (off + (CHAIN + (V / 16384 + 32) * U) * G.abs()) @ w.abs()),
+                              (dw, G.t() @ x, (off + (CHAIN + (M / 16384 + 32) * U) * G.abs()).t() @ x.abs())):
         _near(got, exact, bound + HALF_STEP["bf16"] * (exact.abs() + bound) + 2.0 ** -126, "gradient")
         assert exact.norm() > 4 * bound.norm() or V == 1 << 24 and got is dw
 
