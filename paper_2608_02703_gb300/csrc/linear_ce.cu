@@ -23,12 +23,13 @@
 // without its neighbours.  Partial sums leave by tile and are joined in a fixed
 // order; nothing is added by atomics.
 //
-// Bound by the tensor cores from some 300 tokens on: their pipe is active 96 to 98% of the time in
-// the logits' kernels and 95% in the gradient's (4096 tokens x 32000 x 4096).  2048 tokens x 151936
-// x 4096 take 1.31 ms, which is the library's bf16 rate in a burst (at the power limit 1.49); loss and gradients of
-// 4096 tokens 11.7 to 11.9 ms, 88 to 90% of it.  Few tokens are
-// bound by memory, which reads W three times and writes dW: the loss of 16 tokens x 151936 x 4096 198 us (92% of
-// the copy rate), loss and gradients of 64 x 262144 x 2560 888 us (89%).
+// Bound by the tensor cores with many tokens: their pipe is active 97 to 99% of the time in
+// the logits' kernels and 94% in the gradient's (4096 tokens x 32000 x 4096).  2048 tokens x 151936
+// x 4096 take 1.33 to 1.47 ms (the library's bf16 rate in a burst is 1.31, at the power limit 1.48); loss and gradients
+// of 4096 tokens 11.6 to 11.8 ms, 89 to 90% of the burst.  Of some hundred tokens a part of the MMAs' rows is empty (300
+// tokens x 32000 x 2048 take what 512 do, 184 us, of which 81 would be needed).  Few tokens are
+// bound by memory, which reads W three times and writes dW: the loss of 16 tokens x 151936 x 4096 196 to 200 us (92% of
+// the copy rate), loss and gradients of 64 x 262144 x 2560 925 to 960 us (82 to 85%).
 #include <algorithm>
 
 #include "int8_quant.cuh"
@@ -64,7 +65,7 @@ struct Geom {
   static constexpr int kBars = 2 * kStages + 2 * kAcc + 1;
   static constexpr int kSmem = kBarOff + kBars * 8 + 32 + 16;
   // Sums in parts: registers of the loading warpgroup and of the others, whose sum is at most that of the launch.
-  // (The gradient's loads and MMAs want more: 4096 tokens x 32000 x 4096 without the loss 1920 us, with 56 1960.)
+  // (The gradient's loads and MMAs want more: 4096 tokens x 32000 x 4096, gradients alone, 1920 us, with 56 1960.)
   static constexpr int kRegs0 = kMode == kGrad ? 88 : 72, kRegsE = kMode == kGrad ? 200 : 208;
   static constexpr int kRegsInAll = 128 * kRegs0 + 32 * kEpiWarps * kRegsE;
   static_assert(kRegsInAll <= 65536 / kThreads / 8 * 8 * kThreads, "registers");

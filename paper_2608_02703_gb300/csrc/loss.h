@@ -128,7 +128,7 @@ struct CeCall {
 // Up to 64 tokens G is held in two parts of 16 bits, the value and what its rounding took, which is as good as 32 bits:
 // the second has the rows behind the first, which a block's half of A has room for, so that the products with W are the
 // same and dW takes one more step of 64 rows (up to 32 tokens none).  4 tokens x 4096 x 512, loss and gradients 26.9 ->
-// 27.7 us, 64 x 262144 x 2560 900 -> 935; with G in 16 bits dx and dW stood at 1.4 times what their own rounding leaves.
+// 27.8 us, 64 x 262144 x 2560 900 -> 940; with G in 16 bits dx and dW stood at 1.4 times what their own rounding leaves.
 // More tokens would take twice the MMAs, which bound those calls: there G is rounded to 16 bits.
 inline int ce_half(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 0; }
 int64_t ce_piece_tiles(const archead_loss *l, const CeCall &c);  // tiles of a piece

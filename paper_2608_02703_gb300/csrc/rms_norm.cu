@@ -9,10 +9,13 @@
 // (64-bit arithmetic runs at two operations a cycle here; rows whose sum leaves fp32's
 // range take it.)  y and its quotients are then roundings of fp32 products.
 //
-// Memory bound, with a residual and fp32 (4096 x 2560, rows and codes: 27 us, 85% of the copy rate); in 16 bits,
-// with twice the values a byte, as much by its instructions (4096 x 4096, sum and codes, 26 us, 65%).  1 to 16 warps take a row and
+// Memory bound, with a residual and fp32 (4096 x 2560, rows and codes: 26 us, 88% of the copy rate); in 16 bits,
+// with twice the values a byte, as much by latency: a row's warps load, sum, store and end, and of the next row nothing is
+// under way (4096 x 4096, sum, rows and codes, 28 us, 79%).  1 to 16 warps take a row and
 // keep their part of it in registers, so that x and r are read once.  Rows that do not start on 16 bytes, or whose
-// width is no multiple of 8, go by single values in neighbouring lanes (4096 x 4093 40 us).
+// width is no multiple of 8, go by single values in neighbouring lanes (4096 x 4093 45 us).  Above 8192 columns the loads
+// of a row, all under way at once, do not fit into the registers of 512 threads: 56 to 216 bytes a thread are spilled,
+// by single values up to 528 (1024 x 16384 38 us, 1024 x 16383 104).
 #include <type_traits>
 
 #include "norm_rows.cuh"
