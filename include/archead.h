@@ -636,8 +636,9 @@ ARCHEAD_API archead_status archead_rms_norm_backward(archead_norm *norm, const a
  *   from the lse of the forward with the same arguments.  dx [M][d] and dw [V][d]
  *   are of x's type, each rounded once from fp32 sums; one of them may be NULL (a
  *   frozen head, or frozen states).  Up to 64 tokens G goes into the products in two parts of 16 bits (an error of
- *   half a step of half a step of the type in each of its elements), with more rounded to 16 bits (half a step, which
- *   leaves dx and dw at some 1.4 times what their own rounding does); in fp16 times a power of two by the largest
+ *   half a step of half a step of the type in each of its elements), with more rounded to 16 bits (half a step; what
+ *   that takes at a target is added to dx, and dw stands at some 1.2 to 1.6 times what its own rounding leaves); in
+ *   fp16 times a power of two by the largest
  *   |grad_ce|, so that no less than 2^-39 of that is lost.  Logits are computed again, in pieces of the
  *   vocabulary.  Tokens that are ignored, or whose grad_ce is 0, have dx 0 and take
  *   no part (whatever their rows of x hold); a token whose target was out of range

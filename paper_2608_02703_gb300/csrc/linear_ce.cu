@@ -674,8 +674,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int64_t at = (int64_t)t - base;
             const int hit = t >= 0 && at >= 0 && at < 32 ? (int)at : -1;
             if (__any_sync(0xffffffffu, hit >= 0)) {
+              float at_target = 0.f;
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] -= j == hit ? f : 0.f;
+              for (int j = 0; j < 32; ++j) {
+                v[j] -= j == hit ? f : 0.f;
+                at_target = j == hit ? v[j] : at_target;
+              }
+              if (!kTwo && hit >= 0)
+                p.at.rest[row] = at_target - (p.fp16 ? __half2float(__float2half_rn(at_target))
+                                                     : __bfloat162float(__float2bfloat16_rn(at_target)));
             }
             if (!all_live || p.V - base < 32) {
               const int lim = live ? (int)max((int64_t)0, min((int64_t)32, p.V - base)) : 0;

@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(kFinishTokens *kFinishLanes) ce_finish_kernel(
 }
 
 // dx's rows: the sum of the splits, in order (and of G's second part, in rows of its own), without the
-// factors' scale; zeros for tokens that do not count.  A thread takes four columns.
+// factors' scale, and, of a G in one part, what its rounding took at the target; zeros for tokens that do not
+// count.  A thread takes four columns.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) ce_dx_kernel(const CeDxParams p) {
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
@@ -229,6 +230,24 @@ __global__ void __launch_bounds__(kThreads) ce_dx_kernel(const CeDxParams p) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) t.x += v[j].x, t.y += v[j].y, t.z += v[j].z, t.w += v[j].w;
     }
+  }
+  const int target = place >= 0 && p.half == 0 ? p.at.target[place] : -1;
+  if (target >= 0) {
+    const float rest = p.at.rest[place];
+    const T *w = static_cast<const T *>(p.w) + target * p.ldw + k;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (k + 4 <= p.d) {  // (w's rows start on 16 bytes)
+      const uint2 raw = *reinterpret_cast<const uint2 *>(w);
+      T h[4];
+      memcpy(h, &raw, 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = to_f32(h[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + i < p.d) x[i] = to_f32(w[i]);
+    }
+    t.x += rest * x[0], t.y += rest * x[1], t.z += rest * x[2], t.w += rest * x[3];
   }
   T *out = static_cast<T *>(p.dx) + m * p.ld + k;
   const float x[4] = {t.x * unscale, t.y * unscale, t.z * unscale, t.w * unscale};

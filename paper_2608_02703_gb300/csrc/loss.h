@@ -37,6 +37,7 @@ struct CeScratch {
   int *target;      // [rows] target, or -1 where it is not a vocabulary row
   float *lse;       // [rows]
   float *factor;    // [rows] grad_ce times header->scale
+  float *rest;      // [rows] what rounding took of G at the target (G in one part)
   uint16_t *x;      // panels of 64 columns: [x_pitch / 64][rows][64]
   float2 *part;     // [CeParts][rows]
   float *tlogit;    // [rows]
@@ -100,7 +101,8 @@ cudaError_t launch_ce_finish(const CeFinishParams &p, cudaStream_t s);
 
 struct CeDxParams {
   void *dx;
-  int64_t M, ld, rows;
+  const void *w;
+  int64_t M, ld, ldw, rows;
   int d, pitch, splits;
   int half;  // see CeCall
   bool fp16, vec;
@@ -129,7 +131,9 @@ struct CeCall {
 // the second has the rows behind the first, which a block's half of A has room for, so that the products with W are the
 // same and dW takes one more step of 64 rows (up to 32 tokens none).  4 tokens x 4096 x 512, loss and gradients 26.9 ->
 // 27.8 us, 64 x 262144 x 2560 900 -> 940; with G in 16 bits dx and dW stood at 1.4 times what their own rounding leaves.
-// More tokens would take twice the MMAs, which bound those calls: there G is rounded to 16 bits.
+// More tokens would take twice the MMAs, which bound those calls: there G is rounded to 16 bits.  Half of what a row of G
+// weighs stands at its target; what rounding took there goes into dx by itself, as a multiple of the target's row of W (M d
+// products).
 inline int ce_half(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 0; }
 int64_t ce_piece_tiles(const archead_loss *l, const CeCall &c);  // tiles of a piece
 int ce_dx_splits(const archead_loss *l, int64_t M, int64_t V, int64_t d, bool want_dw);

@@ -38,6 +38,7 @@ void lay_out(archead_loss *l, char *base, size_t *bytes) {
   place(a.lse, 4 * rows);
   place(a.factor, 4 * rows);
   place(a.tlogit, 4 * rows);
+  if (l->gradient) place(a.rest, 4 * rows);
   place(a.x, 2 * rows * up(l->max_hidden, kCeStep));
   place(a.part, (int64_t)sizeof(float2) * ce_most_parts(rows, tiles, l->clusters));
   if (l->gradient) {
@@ -246,6 +247,8 @@ archead_status archead_linear_ce_backward(archead_loss *loss, const void *x, con
   if (dx) {
     CeDxParams f{};
     f.dx = dx;
+    f.w = w;
+    f.ldw = ldw;
     f.M = M;
     f.ld = lddx;
     f.rows = p.rows;

@@ -171,3 +171,32 @@ def test_gradients_of_few_tokens_are_rounded_once(M, V, d, ignored, dtype):
     for got, exact, bound in ((dx, G @ ww, (off + chain * G.abs()) @ ww.abs()), (dw, G.t() @ xx, (off + CHAIN / 64 * G.abs()).t() @ xx.abs())):
         rounding = (exact.to(got.dtype).double() - exact).norm()
         assert (got.double() - exact).norm() <= rounding + 2 * (bound + TINY[dtype]).norm()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("M,d,ldx", [(65, 512, 512), (200, 513, 514), (300, 510, 510), (1000, 768, 768)], ids=str)
+def test_dx_of_more_tokens_keeps_what_its_targets_weigh(M, d, ldx, dtype):
+    """Logits of 0: p is 1 / 4096 in all columns, and G the same but at the target, where nearly all of its weight is.  G is
+    rounded to 16 bits: alike in the other columns, half a step of what they sum up to; at the target what rounding took
+    is added to dx.  So dx is off by its own rounding, but for that (see the test before)."""
+    torch = _torch()
+    V = 4096
+    gen = torch.Generator(device="cuda").manual_seed(81)
+    x = torch.zeros((M, ldx), dtype=_dtype(dtype), device="cuda")[:, :d]
+    w = torch.empty((V, (d + 7) // 8 * 8), dtype=_dtype(dtype), device="cuda")[:, :d]
+    w.copy_(torch.randn((V, d), generator=gen, device="cuda"))
+    t = torch.randint(0, V, (M,), generator=gen, device="cuda").to(torch.int32)
+    t[::5] = IGNORED
+    t[1], t[2] = 0, V - 1
+    g = 0.5 + torch.rand(M, generator=gen, device="cuda")
+    dx = _run(x, w, t, g)[2]
+    live = (t != IGNORED).double()[:, None]
+    ww, gg = w.double(), g.double()[:, None] * live
+    at_target, even = ww[t.clamp_min(0).long()], ww.sum(dim=0, keepdim=True) / V
+    exact = gg * (even - at_target)
+    # p within 2^-15 of itself; sums of 4096 products in one, cut short by 256 * 2^-23 of their absolute terms at most,
+    # and added with some 40 roundings.
+    bound = gg * ((2.0 ** -15 + HALF_STEP[dtype]) * even.abs()
+                  + (2.0 ** -15 + 40 * U) * (ww.abs().sum(dim=0, keepdim=True) / V + at_target.abs()) + 2.0 ** -24 * at_target.abs())
+    rounding = (exact.to(dx.dtype).double() - exact).norm()
+    assert (dx.double() - exact).norm() <= rounding + 2 * (bound + TINY[dtype]).norm()
